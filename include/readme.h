@@ -25,6 +25,9 @@
  *     readme_ungroup          rows back to token order
  *     readme_moe_ffn_stack    L stacked pre-norm residual layers in grouped
  *                             order (routing and grouping done once)
+ * Attention over tokens already seen, for the router and a backbone's own
+ * layers: readme_kv_write, readme_attention_kv, readme_kv_read (a key/value
+ * cache in 8 bits).
  *
  * Conventions for every call:
  *   - Arrays are DEVICE pointers owned by the caller, row-major, contiguous.
@@ -67,6 +70,12 @@ typedef int32_t readme_status;
 typedef int32_t readme_dtype;
 #define README_F32 0
 #define README_BF16 1
+
+/* Codes of the 8-bit key/value cache (readme_kv_write). */
+typedef int32_t readme_kv_type;
+#define README_KV_I8 0   /* integers -127 .. 127 */
+#define README_KV_E4M3 1 /* floating point, 3 mantissa bits, up to 448 (OCP E4M3) */
+#define README_KV_BLOCK 64 /* tokens of a cache block, and of one scale */
 
 #define README_MAX_EXPERTS 256
 #define README_MAX_PERMANENT_SLICES 16
@@ -763,6 +772,104 @@ readme_status readme_rope(int64_t T, int32_t H, const int32_t *pos, void *x, int
 readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int32_t *pos,
                                       const void *q, const void *k, const void *v,
                                       int64_t ld_in, void *o, int64_t ld_out, void *stream);
+
+/*
+ * The key/value cache in 8 bits: keys and values of earlier tokens, so that a
+ * step computes only its new ones.
+ *
+ * A cache is two device arrays that the caller owns, a pool of n_blocks
+ * blocks of README_KV_BLOCK = 64 tokens of Hk heads of D dims:
+ *   codes  [n_blocks][Hk][2][64 D]  bytes, 16-byte aligned
+ *   scales [n_blocks][Hk][2]        fp32, 8-byte aligned
+ * (readme_kv_codes_bytes, readme_kv_scales_bytes); [..][0] keys, [..][1]
+ * values.  A value is its code times the scale of its (block, head, key or
+ * value).  Token slot t, dim d of the keys is byte
+ *   ((t / 32) (D / 16) + d / 16) 512 + (t % 32) 16 + d % 16,
+ * of the values byte ((t / 32) D + d) 32 + t % 32.  README_KV_I8 stores code c
+ * as the byte c + 128, README_KV_E4M3 its own byte.
+ *
+ * All three calls say which tokens they are about in the same way:
+ *   offsets [R+1] int32  request r's rows of the call are [offsets[r],
+ *                        offsets[r+1]), non-decreasing from 0 and at most T
+ *                        (empty requests allowed).  Rows from offsets[R] on
+ *                        belong to no request: not read, not written.
+ *   lens    [R]   int32  its tokens in the cache, the call's among them: with
+ *                        n_r rows, row i is at position lens[r] - n_r + i.
+ *   table   [R][max_blocks] int32  the pool block of positions 64 j .. 64 j + 63
+ *                        is table[r][j].  An entry outside [0, n_blocks), like
+ *                        a position outside [0, 64 max_blocks), is absent.
+ * Positions of request r are its own numbering.  Two requests may share blocks
+ * that no call writes; a block that one call writes through two table entries
+ * ends up with unspecified contents.  Malformed offsets or lens give
+ * unspecified values, never an access outside the arrays.
+ *
+ * readme_kv_write -- the call's rows of K and V into the cache:
+ *   k, v [T][ld] dt (bf16 or fp32), head h at columns D h .. D h + D - 1.
+ *   Per (block, head, K or V) with rows x from this call, QMAX = 127 (I8) or
+ *   448 (E4M3) and need = fp32(max |x| / QMAX):
+ *     scale = max(need, 2^-100) if none of the block's tokens precedes the
+ *             call's, else scale * 2^k with the least k >= 0 for which it is
+ *             at least need; the earlier codes c become round(c 2^-k);
+ *     code  = round(x / scale), the exact quotient;
+ *   both to the nearest code, ties to even.  However often a block grows an
+ *   earlier value is off by less than one step of I8's final scale.  If x
+ *   holds an infinity or a NaN, or the earlier tokens' scale is not positive
+ *   and finite, the scale becomes NaN: every value read from that (block,
+ *   head, K or V) is NaN until its first token is written again.  Rows at
+ *   absent positions are dropped.  Writing the same rows again changes
+ *   nothing.
+ *
+ * readme_kv_read -- the rows back: k, v [T][ld] dt (outputs), value = code *
+ *   scale in fp32, rounded once to dt; zeros at absent positions.  Reading
+ *   tokens other than the last ones takes lens cut off after them.
+ *
+ * readme_attention_kv -- attention of query rows over the cache (write the
+ *   call's own keys and values first):
+ *     o[i]_g = sum_j w_ij v[j]_h / sum_j w_ij,  w_ij = exp(scale q[i]_g . k[j]_h - m_i)
+ *   for query head g, h = g / (H / Hk), over the cached tokens j < lens[r]
+ *   of the row's request; if causal only j <= p, the row's position; with
+ *   window > 0 only j > p - window; never absent ones.  A row that sees no
+ *   token is zeros.  Scores, running softmax and sums in fp32; a row of q
+ *   enters scaled by a power of two in fp16, exactly down to 2^-28 of its
+ *   largest element, the codes exactly, the weights rounded to fp16 (2^-11 of
+ *   themselves, 2^-32 below 2^-21), so o is the exact result up to about
+ *   2^-11 of the largest |v| the row sees plus its rounding to bf16.  The
+ *   order of the sums depends on the sizes and lens, never on timing.
+ *   A row of q with an infinity or a NaN gives an unspecified row; a NaN scale
+ *   gives NaN in the rows that see any of its tokens.
+ *   q [T][ld_q] bf16 (head g at columns D g ..), o [T][ld_o] bf16 out, causal
+ *   0 or 1, window >= 0, scale > 0 and finite; workspace >=
+ *   readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks) bytes,
+ *   contents unspecified before and after.  Calls in flight together need
+ *   workspaces of their own.  o must not overlap q.
+ *
+ * All require D of 64, 128 or 256, 1 <= Hk <= 65535, H a multiple of Hk,
+ * R <= 2^22, T H / Hk <= 2^27, row strides at least the row's width and 16-byte
+ * multiples, arrays of rows 16-byte aligned; T = 0 enqueues nothing, else
+ * R >= 1, max_blocks >= 1 and n_blocks >= 1.  The size queries return 0 for
+ * arguments outside that set.
+ */
+size_t readme_kv_codes_bytes(int64_t n_blocks, int32_t Hk, int32_t D);
+size_t readme_kv_scales_bytes(int64_t n_blocks, int32_t Hk);
+readme_status readme_kv_write(readme_kv_type kt, readme_dtype dt, int64_t T, int32_t R, int32_t Hk,
+                              int32_t D, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                              const int32_t *offsets, const int32_t *lens, const int32_t *table,
+                              int64_t max_blocks, int64_t n_blocks, void *codes, float *scales,
+                              void *stream);
+readme_status readme_kv_read(readme_kv_type kt, readme_dtype dt, int64_t T, int32_t R, int32_t Hk,
+                             int32_t D, const int32_t *offsets, const int32_t *lens,
+                             const int32_t *table, int64_t max_blocks, int64_t n_blocks,
+                             const void *codes, const float *scales, void *k, int64_t ld_k,
+                             void *v, int64_t ld_v, void *stream);
+size_t readme_attention_kv_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk, int32_t D,
+                                           int64_t max_blocks);
+readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                  int32_t D, const void *q, int64_t ld_q, const int32_t *offsets,
+                                  const int32_t *lens, const int32_t *table, int64_t max_blocks,
+                                  int64_t n_blocks, const void *codes, const float *scales,
+                                  float scale, int32_t causal, int64_t window, void *o,
+                                  int64_t ld_o, void *workspace, size_t workspace_bytes,
+                                  void *stream);
 
 #ifdef __cplusplus
 }

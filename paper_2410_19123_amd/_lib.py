@@ -17,6 +17,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libreadme.so")
 
 README_F32, README_BF16 = 0, 1
+README_KV_I8, README_KV_E4M3 = 0, 1
+README_KV_BLOCK = 64
 README_MAX_EXPERTS = 256
 README_MAX_PERMANENT_SLICES = 16
 
@@ -91,6 +93,15 @@ SIGNATURES = {
     "readme_request_positions": (_I32, [_I64, _I32, _P, _P, _P]),
     "readme_rope": (_I32, [_I64, _I32, _P, _P, _I64, _P]),
     "readme_attention_causal": (_I32, [_I64, _I32, _I32, _P, _P, _P, _P, _I64, _P, _I64, _P]),
+    "readme_kv_codes_bytes": (_SZ, [_I64, _I32, _I32]),
+    "readme_kv_scales_bytes": (_SZ, [_I64, _I32]),
+    "readme_kv_write": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P,
+                               _I64, _I64, _P, _P, _P]),
+    "readme_kv_read": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _P, _P, _I64, _I64, _P, _P,
+                              _P, _I64, _P, _I64, _P]),
+    "readme_attention_kv_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I64]),
+    "readme_attention_kv": (_I32, [_I32, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P, _I64,
+                                   _I64, _P, _P, _F, _I32, _I64, _P, _I64, _P, _SZ, _P]),
 }
 
 # Workspace regions of readme_router_tf (README_RTF_*).
@@ -755,6 +766,120 @@ def readme_attention_causal(q, k, v, pos, H: int, R: int = 1, o=None):
     _dev(q, k, v, pos, o)
     _call("readme_attention_causal", T, H, R, _p(pos), _p(q), _p(k), _p(v), ld, _p(o),
           o.shape[1], _stream(q.device))
+    return o
+
+
+# --- the 8-bit key/value cache ------------------------------------------------
+
+def readme_kv_cache(n_blocks: int, Hk: int, D: int, device):
+    """A cache's (codes, scales): uint8 [n_blocks][Hk][2][64 D] and fp32
+    [n_blocks][Hk][2], not initialised (a block is before it is read)."""
+    codes = torch.empty((n_blocks, Hk, 2, README_KV_BLOCK * D), dtype=torch.uint8, device=device)
+    return codes, torch.empty((n_blocks, Hk, 2), dtype=torch.float32, device=device)
+
+
+def readme_kv_codes_bytes(n_blocks: int, Hk: int, D: int) -> int:
+    return int(load().readme_kv_codes_bytes(n_blocks, Hk, D))
+
+
+def readme_kv_scales_bytes(n_blocks: int, Hk: int) -> int:
+    return int(load().readme_kv_scales_bytes(n_blocks, Hk))
+
+
+def _kv_rows(t, T: int, width: int, what: str) -> int:
+    """Row stride of rows [T][>= width] whose columns are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("libreadme takes device tensors")
+    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != width or t.stride(1) != 1:
+        raise ValueError(f"{what} must be [{T}][{width}] rows with contiguous columns")
+    return t.stride(0) if T > 1 else max(t.stride(0), width)
+
+
+def _kv_cache_args(offsets, lens, table, codes, scales):
+    """(R, Hk, D, max_blocks, n_blocks) of a cache and the call's requests."""
+    _dev(offsets, lens, table, codes, scales)
+    for t, what in ((offsets, "offsets"), (lens, "lens"), (table, "table")):
+        if t.dtype != torch.int32:
+            raise ValueError(f"{what} must be int32")
+    if codes.dtype != torch.uint8 or codes.dim() != 4 or codes.shape[2] != 2 or \
+            codes.shape[3] % README_KV_BLOCK:
+        raise ValueError("codes must be uint8 [n_blocks][Hk][2][64 D]")
+    if scales.dtype != torch.float32 or scales.shape != codes.shape[:3]:
+        raise ValueError("scales must be fp32 [n_blocks][Hk][2]")
+    R = lens.shape[0]
+    if offsets.shape != (R + 1,) or lens.dim() != 1 or table.dim() != 2 or table.shape[0] != R:
+        raise ValueError("offsets [R+1], lens [R] and table [R][max_blocks] disagree")
+    return R, codes.shape[1], codes.shape[3] // README_KV_BLOCK, table.shape[1], codes.shape[0]
+
+
+def _kv_call(device, name: str, args, *tensors) -> None:
+    """The call on the device its tensors are on, which has to be one."""
+    for t in tensors:
+        if t.device != device:
+            raise ValueError("tensors on more than one device")
+    with torch.cuda.device(device):
+        _call(name, *args, _stream(device))
+
+
+def readme_kv_write(kt: int, k, v, offsets, lens, table, codes, scales) -> None:
+    """The call's rows k, v ([T][Hk D], bf16 or fp32; slices of wider rows
+    allowed) into the cache, as 8-bit codes and one scale per block and head."""
+    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    T = k.shape[0]
+    ld_k, ld_v = _kv_rows(k, T, Hk * D, "k"), _kv_rows(v, T, Hk * D, "v")
+    if v.dtype != k.dtype:
+        raise ValueError("k and v dtypes disagree")
+    _kv_call(codes.device, "readme_kv_write",
+             (kt, _dt(k), T, R, Hk, D, _p(k), ld_k, _p(v), ld_v, _p(offsets), _p(lens), _p(table),
+              mb, nb, _p(codes), _p(scales)), k, v, offsets, lens, table, scales)
+
+
+def readme_kv_read(kt: int, offsets, lens, table, codes, scales, k=None, v=None, T: int = None,
+                   dtype=torch.bfloat16):
+    """Cached rows back; returns (k, v) [T][Hk D].  Rows past offsets[R] keep
+    what they held."""
+    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    if k is None or v is None:
+        rows = T if T is not None else (k if k is not None else v).shape[0]
+        dtype = k.dtype if k is not None else v.dtype if v is not None else dtype
+        k = k if k is not None else torch.empty((rows, Hk * D), dtype=dtype, device=codes.device)
+        v = v if v is not None else torch.empty((rows, Hk * D), dtype=dtype, device=codes.device)
+    T = k.shape[0]
+    ld_k, ld_v = _kv_rows(k, T, Hk * D, "k"), _kv_rows(v, T, Hk * D, "v")
+    if v.dtype != k.dtype:
+        raise ValueError("k and v dtypes disagree")
+    _kv_call(codes.device, "readme_kv_read",
+             (kt, _dt(k), T, R, Hk, D, _p(offsets), _p(lens), _p(table), mb, nb, _p(codes),
+              _p(scales), _p(k), ld_k, _p(v), ld_v), k, v, offsets, lens, table, scales)
+    return k, v
+
+
+def readme_attention_kv_workspace_bytes(T: int, R: int, H: int, Hk: int, D: int,
+                                        max_blocks: int) -> int:
+    return int(load().readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks))
+
+
+def readme_attention_kv(kt: int, q, offsets, lens, table, codes, scales, H: int, scale=None,
+                        causal: bool = True, window: int = 0, o=None, workspace=None):
+    """Attention of query rows q ([T][H D] bf16; slices of wider rows allowed)
+    over the cache; scale defaults to 1 / sqrt(D).  Returns o [T][H D]."""
+    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    T = q.shape[0]
+    if q.dtype != torch.bfloat16 or (o is not None and o.dtype != torch.bfloat16):
+        raise ValueError("q and o must be bf16")
+    if o is None:
+        o = torch.empty((T, H * D), dtype=torch.bfloat16, device=q.device)
+    ld_q, ld_o = _kv_rows(q, T, H * D, "q"), _kv_rows(o, T, H * D, "o")
+    if workspace is None:
+        ws = readme_attention_kv_workspace_bytes(T, R, H, Hk, D, mb)
+        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=q.device)
+    _dev(workspace)
+    scale = D ** -0.5 if scale is None else scale
+    _kv_call(codes.device, "readme_attention_kv",
+             (kt, T, R, H, Hk, D, _p(q), ld_q, _p(offsets), _p(lens), _p(table), mb, nb, _p(codes),
+              _p(scales), float(scale), int(bool(causal)), int(window), _p(o), ld_o, _p(workspace),
+              workspace.numel() * workspace.element_size()), q, o, offsets, lens, table, scales,
+             workspace)
     return o
 
 

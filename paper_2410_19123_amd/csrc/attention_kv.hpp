@@ -1,0 +1,148 @@
+// Shared by the two attention kernels over the 8-bit cache
+// (attention_kv_rows.hip: few query rows, attention_kv_tiles.hip: many).
+//
+// For a query row i (a token and one of the G query heads of a key head) at
+// position p and the keys j it sees (j < len; j <= p if causal; j > p - window)
+//   o_i = sum_j w_ij v_j / sum_j w_ij,   w_ij = exp(scale <q_i, k_j>)
+// with k_j = ks c_j, v_j = vs d_j: codes c, d of at most 8 significant bits, so
+// exact in fp16, and one scale per block of 64 tokens.
+//   Scores: q_i is scaled by a power of two so that its largest element is in
+//   [2^14, 2^15) and taken in fp16, exactly for elements down to 2^-28 of the
+//   largest (bf16 carries 8 bits, fp16 11); products of codes add up in fp32, and
+//   score = (scale log2e 2^-x ks) * sum, one factor per row and block.
+//   Softmax: running maximum m and sum l per row in fp32, weights 2^(score - m).
+//   m is raised, and the sums rescaled, only when a block's maximum passes it by
+//   more than kLazy, so weights reach 2^kLazy at most and most blocks skip the
+//   rescaling.
+//   Values: the block's vs goes into the exponent as r = vs / vref, vref the
+//   largest scale so far (the accumulators are in units of vref), so it costs
+//   nothing per weight: p = 2^(score - m + log2 r + kUp) in fp16 times the codes,
+//   added in fp32; l adds (sum of the block's p in fp32) / r.  p rounds to 11 bits
+//   (at most 2^-11 of itself; against bf16 weights, 8 bits, an eighth of the error for
+//   the same instructions), and kUp keeps weights down to 2^-21 out of fp16's
+//   subnormals; smaller ones are off by at most 2^-32.  o is therefore within
+//   about 2^-11 max|v| of the exact result before its own rounding to bf16.
+#pragma once
+
+#include "kv_cache.hpp"
+
+namespace readme {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2v __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+constexpr float kLazy = 8.0f;  // log2 of the largest weight
+constexpr float kUp = 7.0f;    // 2^(kLazy + kUp) = 32768 < 65504, fp16's largest
+
+// Four codes to two fp16 pairs, exact.  int8 bytes are code + 128: 0x64xx is
+// 1024 + xx in fp16, less 1152.
+template <int KT>
+__device__ __forceinline__ void cvt4(uint32_t w, uint32_t& a, uint32_t& b) {
+    if constexpr (KT == README_KV_I8) {
+        const f16x2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+        const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(w, 0x64646464u, 0x00050004u));
+        const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(w, 0x64646464u, 0x00070006u));
+        a = __builtin_bit_cast(uint32_t, lo - off);
+        b = __builtin_bit_cast(uint32_t, hi - off);
+    } else {
+        a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+        b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true));
+    }
+}
+template <int KT>
+__device__ __forceinline__ f16x8 cvt8(uint32_t w0, uint32_t w1) {
+    u32x4v r;
+    uint32_t a, b, c, d;
+    cvt4<KT>(w0, a, b);
+    cvt4<KT>(w1, c, d);
+    r[0] = a;
+    r[1] = b;
+    r[2] = c;
+    r[3] = d;
+    return __builtin_bit_cast(f16x8, r);
+}
+
+// Bytes of a 16-token piece at or past `n` (tokens that are not in the cache)
+// to zero: a byte never written may be an e4m3 NaN, which a weight of zero
+// would not silence.
+__device__ __forceinline__ uint4 keep_tokens(uint4 w, int n) {
+    uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = n - 4 * i;
+        if (k <= 0) v[i] = 0u;
+        else if (k < 4) v[i] &= 0xffffffffu >> (8 * (4 - k));
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// Two weights to fp16, nearest even.
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const f32x2v p = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2));
+}
+
+// A block's value scale against the running largest: log2 r and 1 / r.  Below
+// 2^-40 the block's values are under fp32's rounding of the rest and r stays
+// there; a NaN scale passes through the weights (a row that gives the block none
+// must not see it: 0 / r stays 0).
+__device__ __forceinline__ void value_ratio(float vs, float vref, float& log_r, float& inv_r) {
+    const float r = vs / vref;
+    const float c = r < 9.094947017729282e-13f ? 9.094947017729282e-13f : r;
+    log_r = __builtin_amdgcn_logf(c);
+    inv_r = c > 0.0f ? 1.0f / c : 1.0f;
+}
+
+// Query rows as fp16 matrix operands.  Each lane holds elements of one row in
+// x; `big` is the largest magnitude in the row.  Returns 2^x and its inverse;
+// a row of zeros (or one too small to matter) keeps a bounded power.
+__device__ __forceinline__ void row_power(float big, float& up, float& down) {
+    int e = 0;
+    (void)frexpf(big, &e);
+    e = big > 0.0f ? e : 0;
+    e = e < -60 ? -60 : e;
+    up = ldexpf(1.0f, 15 - e);
+    down = ldexpf(1.0f, e - 15);
+}
+
+// What a request asks of the kernels.
+struct KvRequest {
+    int64_t row0;     // its first row in the call
+    int n;            // its rows
+    int len;          // its tokens in the cache
+    int block0;       // first and one past the last block any of its rows sees
+    int block1;
+};
+
+__device__ __forceinline__ KvRequest kv_request(const KvAttnArgs& a, int64_t r) {
+    KvRequest q;
+    int64_t lo, hi;
+    kv_rows(a.c.offsets, a.c.T, r, lo, hi);
+    q.row0 = lo;
+    q.n = (int)(hi - lo);
+    const int64_t cap = a.c.max_blocks * kKvBlock;
+    int64_t len = a.c.lens[r];
+    const int64_t first = len - q.n;
+    int64_t b1 = len < cap ? len : cap;
+    b1 = b1 < 0 ? 0 : (b1 + kKvBlock - 1) / kKvBlock;
+    int64_t b0 = 0;
+    if (a.window > 0 && first - a.window + 1 > 0) b0 = (first - a.window + 1) / kKvBlock;
+    q.len = (int)len;
+    q.block1 = (int)b1;
+    q.block0 = (int)(b0 < b1 ? b0 : b1);
+    return q;
+}
+
+// Keys [lo, hi) that a row at position p sees.
+__device__ __forceinline__ void row_keys(const KvAttnArgs& a, int len, int64_t p, int& lo, int& hi) {
+    int64_t h = a.causal && p + 1 < len ? p + 1 : len;
+    int64_t l = a.window > 0 ? p - a.window + 1 : 0;
+    h = h < 0 ? 0 : h;
+    l = l < 0 ? 0 : (l > h ? h : l);
+    lo = (int)l;
+    hi = (int)h;
+}
+
+}  // namespace readme

@@ -1,0 +1,530 @@
+"""The 8-bit key/value cache on the GPU against its 64-bit oracle: written
+bytes and scales exactly, rows read back exactly, attention within its derived
+bound."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_cache as ok
+
+pytestmark = pytest.mark.gpu
+
+KT = {"i8": 0, "e4m3": 1}
+
+
+def _lib():
+    from paper_2410_19123_amd import _lib
+    return _lib
+
+
+def _i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda:0")
+
+
+def _offsets(new):
+    return np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+
+
+def _table(rng, R, max_blocks, n_blocks):
+    """Blocks in no order; n_blocks >= R * max_blocks."""
+    return rng.permutation(n_blocks)[:R * max_blocks].reshape(R, max_blocks).astype(np.int32)
+
+
+def _rows(rng, T, Hk, D, dtype):
+    """Rows whose sizes differ from row to row (so that blocks grow), with many
+    values halfway between codes (small multiples of powers of two)."""
+    x = rng.standard_normal((T, Hk, D)) * 2.0 ** rng.integers(-2, 3, (T, 1, 1))
+    tie = rng.random((T, Hk, D)) < 0.3
+    x = np.where(tie, rng.integers(-64, 65, (T, Hk, D)) / 32.0, x)
+    return torch.from_numpy(x).to(dtype)
+
+
+class Cache:
+    """One cache on the GPU and in the oracle."""
+
+    def __init__(self, kt, R, Hk, D, max_blocks, seed, spare=2):
+        self.rng = np.random.default_rng(seed)
+        self.kt, self.Hk, self.D = kt, Hk, D
+        n = R * max_blocks + spare
+        self.table = _table(self.rng, R, max_blocks, n)
+        self.ref = ok.new_cache(n, Hk, D)
+        self.codes = torch.from_numpy(ok.to_bytes(kt, self.ref["codes"])).cuda()
+        self.scales = torch.zeros((n, Hk, 2), dtype=torch.float32, device="cuda:0")
+
+    def args(self):
+        return _i32(self.table), self.codes, self.scales
+
+    def write(self, new, lens, dtype, k=None, v=None, pad=0):
+        L = _lib()
+        off, T = _offsets(new), int(sum(new)) + pad
+        if k is None:
+            k = _rows(self.rng, T, self.Hk, self.D, dtype)
+            v = _rows(self.rng, T, self.Hk, self.D, dtype)
+        L.readme_kv_write(KT[self.kt], k.reshape(T, -1).cuda(), v.reshape(T, -1).cuda(), _i32(off),
+                          _i32(lens), *self.args())
+        torch.cuda.synchronize()
+        ok.write(self.kt, self.ref, k.double().numpy(), v.double().numpy(), off, lens, self.table)
+
+    def check(self):
+        np.testing.assert_array_equal(self.scales.cpu().numpy(), self.ref["scales"])
+        got = self.codes.cpu().numpy()
+        np.testing.assert_array_equal(got, ok.to_bytes(self.kt, self.ref["codes"]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+@pytest.mark.parametrize("D,Hk", [(64, 3), (128, 2), (256, 1)])
+def test_write_is_exact(kt, dtype, D, Hk):
+    """Prompts, single tokens, drafts and pieces across block borders, several
+    calls in a row on requests of every length."""
+    c = Cache(kt, 5, Hk, D, 4, seed=D + Hk)
+    lens = np.zeros(5, np.int32)
+    for new in ([1, 63, 64, 65, 130], [1, 1, 1, 1, 1], [5, 0, 3, 62, 1], [60, 2, 70, 0, 1],
+                [1, 1, 1, 1, 1]):
+        lens = lens + np.array(new, np.int32)
+        c.write(new, lens, dtype)
+        c.check()
+
+
+def _random_calls(c, steps, dtype=torch.bfloat16):
+    R, cap = c.table.shape[0], c.table.shape[1] * 64
+    lens = np.zeros(R, np.int64)
+    for _ in range(steps):
+        new = np.minimum(c.rng.integers(0, 90, R), cap - lens)
+        if new.sum() == 0:
+            new[0] = min(1, cap - lens[0])
+        lens = lens + new
+        c.write(new, lens.astype(np.int32), dtype)
+    return lens.astype(np.int32)
+
+
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+def test_write_many_requests(kt):
+    """More requests than a wave holds, many of them empty, several block
+    borders in one run of 64 rows."""
+    c = Cache(kt, 150, 1, 64, 2, seed=7)
+    rng = np.random.default_rng(8)
+    lens = rng.integers(0, 80, 150).astype(np.int32)
+    c.write(lens, lens, torch.bfloat16)
+    c.check()
+    for _ in range(3):
+        new = rng.integers(0, 9, 150) * (rng.random(150) < 0.6)
+        lens = (lens + new).astype(np.int32)
+        c.write(new, lens, torch.bfloat16)
+        c.check()
+
+
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+def test_write_absent_and_foreign_rows(kt):
+    """Absent blocks and positions before the first token or past the table
+    drop their rows; rows past offsets[R] are not read (they are NaN here)."""
+    c = Cache(kt, 4, 2, 64, 2, seed=9)
+    c.table[1, 0] = -1
+    c.table[2, 1] = 1 << 30
+    new, lens = [10, 100, 100, 40], [4, 100, 100, 140]
+    k = _rows(c.rng, 257, 2, 64, torch.float32)
+    v = _rows(c.rng, 257, 2, 64, torch.float32)
+    k[250:] = float("nan")
+    v[250:] = float("nan")
+    c.write(new, lens, torch.float32, k, v, pad=7)
+    c.check()
+
+
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_write_zeros_extremes_and_poison(kt, dtype):
+    """Zero rows, the largest and smallest magnitudes, growth from the floor
+    scale, and infinities and NaN (scale NaN until the block's first token is
+    written again)."""
+    c = Cache(kt, 6, 1, 64, 1, seed=10)
+    k = torch.zeros((12, 1, 64), dtype=dtype)
+    v = _rows(c.rng, 12, 1, 64, dtype)
+    k[2:4] = 3.0e38
+    k[4, 0, 5] = 1e-38
+    k[6, 0, 1] = float("inf")
+    k[8, 0, 2] = float("nan")
+    v[9, 0, 3] = -float("inf")
+    c.write([2] * 6, [2] * 6, dtype, k, v)
+    c.check()
+    assert torch.isnan(c.scales).sum() == 3
+    c.write([2] * 6, [4] * 6, dtype, k.flip(0).clone(), v.flip(0).clone())
+    c.check()
+    x = _rows(c.rng, 18, 1, 64, dtype)
+    c.write([3] * 6, [3] * 6, dtype, x, x)
+    c.check()
+    assert not torch.isnan(c.scales).any()
+
+
+def test_write_again_changes_nothing():
+    c = Cache("e4m3", 3, 2, 128, 3, seed=11)
+    c.write([100, 20, 64], [100, 20, 64], torch.bfloat16)
+    k, v = (_rows(c.rng, 60, 2, 128, torch.bfloat16) for _ in range(2))
+    for _ in range(2):
+        c.write([30, 20, 10], [130, 40, 74], torch.bfloat16, k, v)
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+@pytest.mark.parametrize("D,Hk", [(64, 3), (128, 2), (256, 1)])
+def test_read_is_exact(kt, dtype, D, Hk):
+    """Whole requests, tails and single tokens from random codes and scales,
+    absent blocks as zeros, rows of no request untouched."""
+    L = _lib()
+    c = Cache(kt, 4, Hk, D, 4, seed=D)
+    raw = c.rng.integers(0, 256, c.codes.shape).astype(np.uint8)
+    if kt == "e4m3":
+        raw[(raw & 127) == 127] = 5                  # NaN bytes are never written
+    sc = np.exp2(c.rng.uniform(-20, 5, c.scales.shape)).astype(np.float32)
+    c.codes.copy_(torch.from_numpy(raw))
+    c.scales.copy_(torch.from_numpy(sc))
+    c.ref = {"codes": ok.from_bytes(kt, raw, D), "scales": sc}
+    c.table[3, 1] = -7
+    for new, lens in (([200, 1, 64, 130], [200, 65, 128, 200]), ([0, 3, 256, 5], [9, 1, 256, 70])):
+        off, T = _offsets(new), sum(new) + 3
+        out = [torch.full((T, Hk * D), 77.0, dtype=dtype, device="cuda:0") for _ in range(2)]
+        L.readme_kv_read(KT[kt], _i32(off), _i32(lens), *c.args(), k=out[0], v=out[1])
+        torch.cuda.synchronize()
+        for got, ref in zip(out, ok.read(c.ref, T, off, lens, c.table, 77.0)):
+            want = torch.from_numpy(ref).float().to(dtype).reshape(T, -1)
+            assert torch.equal(got.cpu(), want)
+
+
+def test_rows_of_wider_arrays():
+    """K, V, Q and O as slices of wider rows, on another stream than torch's."""
+    L = _lib()
+    c = Cache("i8", 2, 2, 64, 2, seed=12)
+    T, W = 90, 2 * 64
+    wide = torch.randn(T, 6 * 64 + 4 * 64 + 8, device="cuda:0").bfloat16()
+    q, k, v = wide[:, :256], wide[:, 256:256 + W], wide[:, 256 + W:256 + 2 * W]
+    off, lens = _i32([0, 50, 90]), _i32([50, 40])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        L.readme_kv_write(0, k, v, off, lens, *c.args())
+        ob = torch.full((T, 512), 9.0, dtype=torch.bfloat16, device="cuda:0")
+        L.readme_attention_kv(0, q, off, lens, *c.args(), H=4, o=ob[:, 128:384])
+    s.synchronize()
+    d = Cache("i8", 2, 2, 64, 2, seed=12)
+    L.readme_kv_write(0, k.contiguous(), v.contiguous(), off, lens, *d.args())
+    o = L.readme_attention_kv(0, q.contiguous(), off, lens, *d.args(), H=4)
+    torch.cuda.synchronize()
+    assert torch.equal(c.codes, d.codes) and torch.equal(c.scales, d.scales)
+    assert torch.equal(ob[:, 128:384], o)
+    assert (ob[:, :128] == 9).all() and (ob[:, 384:] == 9).all()
+
+
+# --- attention ----------------------------------------------------------------
+
+def _random_cache(kt, R, Hk, D, max_blocks, seed):
+    """A cache of random codes with value scales over a factor of 2^12."""
+    c = Cache(kt, R, Hk, D, max_blocks, seed)
+    rng = c.rng
+    x = rng.standard_normal(c.ref["codes"].shape)
+    x /= np.abs(x).max((3, 4), keepdims=True) / ok.QMAX[kt]
+    c.ref["codes"] = ok.nearest(kt, x)
+    c.ref["scales"] = (np.exp2(rng.uniform(-2, 2, c.scales.shape)) * 3 / ok.QMAX[kt]).astype(np.float32)
+    c.ref["scales"][..., 1] *= np.exp2(rng.uniform(-8, 4, c.scales.shape[:2])).astype(np.float32)
+    c.codes.copy_(torch.from_numpy(ok.to_bytes(kt, c.ref["codes"])))
+    c.scales.copy_(torch.from_numpy(c.ref["scales"]))
+    return c
+
+
+def _poison_unused(c, lens):
+    """NaN codes (e4m3) and huge ones in every slot no request has reached, NaN
+    scales in every block none has: none of it may be seen."""
+    raw = np.full(c.codes.shape, 0x7f, np.uint8)
+    keep = np.zeros(c.ref["codes"].shape[:1] + (64,), bool)
+    for r, ln in enumerate(lens):
+        for j in range(max(0, int(ln))):
+            b = ok.block_of(c.table, len(keep), r, j)
+            if b >= 0:
+                keep[b, j % 64] = True
+    mask = np.broadcast_to(keep[:, None, None, :, None], c.ref["codes"].shape)
+    byte_mask = ok.to_bytes("i8", mask.astype(np.float64) - 128).astype(bool)
+    good = ok.to_bytes(c.kt, c.ref["codes"])
+    c.codes.copy_(torch.from_numpy(np.where(byte_mask, good, raw)))
+    sc = c.ref["scales"].copy()
+    sc[~keep.any(1)] = np.nan
+    c.scales.copy_(torch.from_numpy(sc))
+
+
+def _attend(c, new, lens, H, causal=True, window=0, scale=None, pad=0, q=None, workspace=None):
+    L = _lib()
+    off, T, D = _offsets(new), int(sum(new)) + pad, c.D
+    if q is None:
+        q = torch.from_numpy(c.rng.standard_normal((T, H, D)) * 1.5).bfloat16()
+    o = torch.full((T, H * D), 55.0, dtype=torch.bfloat16, device="cuda:0")
+    scale = D ** -0.5 if scale is None else scale
+    L.readme_attention_kv(KT[c.kt], q.reshape(T, -1).cuda(), _i32(off), _i32(lens), *c.args(), H=H,
+                          scale=scale, causal=causal, window=window, o=o, workspace=workspace)
+    torch.cuda.synchronize()
+    ref, vmax, zabs = ok.attention(c.ref, q.double().numpy(), off, lens, c.table,
+                                   float(np.float32(scale)), causal, window, 55.0)
+    got = o.cpu().double().numpy().reshape(T, H, D)
+    # bf16's half step of the result; fp16's half step of every weight; the
+    # scores' fp32 sums of D products (D + 8 roundings of at most sum |q||k|
+    # scale, each weight and the sum of weights off by that); exp2 and the
+    # running sums, a few units of fp32
+    delta = (D + 8) * 2.0 ** -24 * zabs + 2.0 ** -18
+    tol = 2.0 ** -8 * np.abs(ref) + ((2.0 ** -11 + 2 * delta) * vmax)[..., None]
+    err = np.abs(got - ref)
+    assert np.isfinite(got).all()
+    worst = (err - tol).max()
+    assert worst <= 0, f"over the bound by {worst}, at {np.unravel_index((err - tol).argmax(), err.shape)}"
+    return got, o
+
+
+CASES = [
+    # new, lens: decode of every length, a block's borders
+    ([1] * 9, [1, 2, 63, 64, 65, 128, 129, 500, 640]),
+    # drafts, empty requests, an empty cache, rows before the first token
+    ([3, 0, 5, 8, 4, 2], [3, 100, 200, 64, 0, 1]),
+    # pieces and prompts
+    ([70, 33, 129], [70, 500, 300]),
+]
+
+
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+@pytest.mark.parametrize("D,Hk,G", [(64, 2, 1), (64, 1, 7), (128, 2, 4), (128, 1, 16), (128, 1, 33),
+                                    (256, 1, 2)])
+@pytest.mark.parametrize("case", range(len(CASES)))
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 100), (False, 0)])
+def test_attention(kt, D, Hk, G, case, causal, window):
+    new, lens = CASES[case]
+    c = _random_cache(kt, len(new), Hk, D, 10, seed=100 + case)
+    _poison_unused(c, lens)
+    got, _ = _attend(c, new, lens, Hk * G, causal, window, pad=2)
+    assert (got[sum(new):] == 55).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_absent_blocks(new):
+    """Blocks absent first, last, between and all: their tokens are not seen,
+    and a row left with none is zeros."""
+    c = _random_cache("e4m3", 5, 2, 128, 4, seed=20)
+    c.table[0, 0] = -1
+    c.table[1, 3] = 1 << 20
+    c.table[2, 1] = -5
+    c.table[3, :] = -1
+    lens = [250, 250, 200, 256, 70]
+    c.table[4, 1] = -1
+    _poison_unused(c, lens)
+    got, _ = _attend(c, [new] * 5, lens, 4)
+    assert (got[3 * new:4 * new] == 0).all()
+    _attend(c, [new] * 5, lens, 4, causal=False)
+    _attend(c, [new] * 5, lens, 4, window=3)
+
+
+def test_attention_lens_past_the_table():
+    c = _random_cache("i8", 2, 1, 64, 2, seed=21)
+    _attend(c, [2, 1], [400, 128], 2, causal=False)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_attention_peaked_and_flat(new):
+    """Scores up to thousands apart (one token takes all) and all equal; a row
+    of zeros; rows of very large and very small q."""
+    c = _random_cache("i8", 2, 1, 128, 8, seed=22)
+    q = torch.randn(2 * new, 4, 128)
+    q[:, 0] *= 300.0
+    q[:, 1] = 0.0
+    q[:, 2] *= 1e-30
+    q[:, 3] *= 1e4
+    _attend(c, [new, new], [512, 301], 4, q=q.bfloat16())
+    _attend(c, [new, new], [512, 301], 4, q=q.bfloat16(), scale=1e-6)
+
+
+@pytest.mark.parametrize("kt", ["i8", "e4m3"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_every_code_value_comes_back(kt, new):
+    """One visible token: the row is that token's values, so every code goes
+    through the value product exactly."""
+    c = Cache(kt, 1, 1, 256, 1, seed=23)
+    vals = np.arange(-127, 128) if kt == "i8" else ok.e4m3_values()
+    vals = np.concatenate([vals[np.isfinite(vals)], np.zeros(8)])[:256]
+    c.ref["codes"][0, 0, 1, :] = np.resize(vals, 256)
+    c.ref["scales"][:] = 1.0
+    c.table[:] = 0
+    c.codes.copy_(torch.from_numpy(ok.to_bytes(kt, c.ref["codes"])))
+    c.scales.copy_(torch.from_numpy(c.ref["scales"]))
+    got, _ = _attend(c, [new], [new], 1, window=1)
+    np.testing.assert_array_equal(got[:, 0], np.broadcast_to(np.resize(vals, 256), (new, 256)))
+
+
+def test_nan_scales_reach_only_their_readers():
+    L = _lib()
+    c = _random_cache("i8", 3, 1, 64, 3, seed=24)
+    lens = [150, 150, 150]
+    for r, half in ((0, 0), (1, 1)):
+        c.scales[int(c.table[r, 1]), 0, half] = float("nan")
+    for new in (1, 90):
+        off = _i32(_offsets([new] * 3))
+        q = torch.randn(3 * new, 64, device="cuda:0").bfloat16()
+        o = L.readme_attention_kv(0, q, off, _i32(lens), *c.args(), H=1).float().view(3, new, 64)
+        pos = torch.arange(150 - new, 150, device="cuda:0")
+        for r in (0, 1):
+            assert torch.isnan(o[r][pos >= 64]).all()
+            assert not torch.isnan(o[r][pos < 64]).any()
+        assert not torch.isnan(o[2]).any()
+        # A window past the block does not see it
+        o = L.readme_attention_kv(0, q, off, _i32(lens), *c.args(), H=1, window=10).float()
+        assert not torch.isnan(o.view(3, new, 64)[:, pos >= 137]).any()
+
+
+@pytest.mark.parametrize("R,lens", [(1, [40000]), (3, [20000, 1, 9000]), (70, None)])
+def test_attention_long_and_uneven(R, lens):
+    """Work split over the keys and joined: against float64 torch on the GPU."""
+    L = _lib()
+    Hk, G, D = 2, 4, 128
+    rng = np.random.default_rng(30 + R)
+    lens = lens or [int(x) for x in np.exp(rng.uniform(0, 8.5, R))]
+    mb = (max(lens) + 63) // 64
+    n = sum((x + 63) // 64 for x in lens)
+    perm = rng.permutation(n)
+    table = np.full((R, mb), -1, np.int32)
+    at = 0
+    for r, x in enumerate(lens):
+        k = (x + 63) // 64
+        table[r, :k] = perm[at:at + k]
+        at += k
+    g = torch.Generator(device="cuda:0").manual_seed(R)
+    codes = torch.randint(1, 256, (n, Hk, 2, 64 * D), generator=g, device="cuda:0",
+                          dtype=torch.int32).to(torch.uint8)
+    scales = torch.rand((n, Hk, 2), generator=g, device="cuda:0") * 0.02 + 0.01
+    q = torch.randn((R, Hk * G * D), generator=g, device="cuda:0").bfloat16()
+    args = (_i32(np.arange(R + 1)), _i32(lens), _i32(table), codes, scales)
+    o = L.readme_attention_kv(0, q, *args, H=Hk * G)
+    again = L.readme_attention_kv(0, q, *args, H=Hk * G)
+    torch.cuda.synchronize()
+    assert torch.equal(o, again)
+    for r, x in enumerate(lens):
+        b = torch.from_numpy(table[r, :(x + 63) // 64]).long().cuda()
+        raw = codes[b].double() - 128
+        kk = raw[:, :, 0].view(-1, Hk, 2, D // 16, 32, 16).permute(1, 0, 2, 4, 3, 5).reshape(Hk, -1, 64, D)
+        vv = raw[:, :, 1].view(-1, Hk, 2, D, 32).permute(1, 0, 2, 4, 3).reshape(Hk, -1, 64, D)
+        sc = scales[b].double().permute(2, 1, 0)
+        kk = (kk * sc[0][..., None, None]).reshape(Hk, -1, D)[:, :x]
+        vv = (vv * sc[1][..., None, None]).reshape(Hk, -1, D)[:, :x]
+        z = torch.matmul(q[r].double().view(Hk, G, D), kk.transpose(1, 2).contiguous()) * D ** -0.5
+        ref = torch.matmul(torch.softmax(z, -1), vv).reshape(-1)
+        vmax = float(vv.abs().max())
+        delta = (D + 8) * 2.0 ** -24 * float((q[r].double().abs().max() * kk.abs().max() * D * D ** -0.5)) + 2.0 ** -18
+        # partial sums of up to 40000 weights in fp32: 64 per block in order,
+        # blocks of a wave after one another, at most 2^-24 each
+        delta += 2.0 ** -24 * (64 + x / 64)
+        tol = 2.0 ** -8 * ref.abs() + (2.0 ** -11 + 2 * delta) * vmax
+        assert ((o[r].double() - ref).abs() <= tol).all(), r
+
+
+# --- together -------------------------------------------------------------------
+
+def test_a_conversation_step_by_step():
+    """Prompts, then single tokens and drafts, as a server runs them: write,
+    attend, and read back, on one cache whose blocks are reused by a new request
+    at the end."""
+    c = Cache("i8", 3, 2, 64, 4, seed=40)
+    lens = np.zeros(3, np.int32)
+    for new in ([70, 1, 130], [1, 1, 1], [1, 1, 1], [4, 60, 2], [1, 0, 1]):
+        lens = lens + np.array(new, np.int32)
+        c.write(new, lens, torch.bfloat16)
+        c.check()
+        _attend(c, new, lens, 4)
+    # Request 2 ends, a new one takes its blocks
+    lens[2] = 0
+    new = [1, 1, 20]
+    lens = lens + np.array(new, np.int32)
+    c.write(new, lens, torch.bfloat16)
+    c.check()
+    _attend(c, new, lens, 4, window=16)
+
+
+def test_a_captured_step_replays():
+    """Write, attend and read in one graph, replayed on other tokens and lengths
+    with eager work between, equal to the eager calls bit for bit; two graphs
+    with workspaces of their own."""
+    L = _lib()
+    R, Hk, G, D, mb = 6, 2, 4, 128, 40
+    rng = np.random.default_rng(41)
+    table = _i32(_table(rng, R, mb, R * mb))
+    base_codes = torch.randint(1, 256, (R * mb, Hk, 2, 64 * D), device="cuda:0",
+                               dtype=torch.int32).to(torch.uint8)
+    base_scales = torch.rand((R * mb, Hk, 2), device="cuda:0") * 0.02 + 0.01
+    codes, scales = base_codes.clone(), base_scales.clone()
+    off = _i32(np.arange(R + 1))
+    lens = _i32(np.ones(R))
+    k, v = (torch.empty((R, Hk * D), dtype=torch.bfloat16, device="cuda:0") for _ in range(2))
+    q = torch.empty((R, Hk * G * D), dtype=torch.bfloat16, device="cuda:0")
+    o = torch.empty_like(q)
+    kb, vb = torch.empty_like(k), torch.empty_like(v)
+
+    def make(ws):
+        def step():
+            L.readme_kv_write(0, k, v, off, lens, table, codes, scales)
+            L.readme_attention_kv(0, q, off, lens, table, codes, scales, H=Hk * G, o=o, workspace=ws)
+            L.readme_kv_read(0, off, lens, table, codes, scales, k=kb, v=vb)
+        return step
+
+    need = L.readme_attention_kv_workspace_bytes(R, R, Hk * G, Hk, D, mb)
+    steps = [make(torch.full((need,), 255, dtype=torch.uint8, device="cuda:0")) for _ in range(2)]
+    inputs = [(torch.randn(R, Hk * D, device="cuda:0"), torch.randn(R, Hk * D, device="cuda:0"),
+               torch.randn(R, Hk * G * D, device="cuda:0"), _i32(ln))
+              for ln in ([1, 64, 65, 700, 2500, 33], [2560, 1, 2, 3, 4, 5], [10] * 6)]
+
+    def load(i):
+        for dst, src in zip((k, v, q, lens), inputs[i]):
+            dst.copy_(src)
+        codes.copy_(base_codes)
+        scales.copy_(base_scales)
+
+    outs = (o, kb, vb, codes, scales)
+    refs = []
+    for i in range(3):
+        load(i)
+        steps[0]()
+        torch.cuda.synchronize()
+        refs.append([t.clone() for t in outs])
+    graphs = []
+    for step in steps:
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            step()
+        torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        torch.cuda.synchronize()
+        graphs.append(graph)
+    for rep in range(2):
+        for i in range(3):
+            for graph in graphs:
+                load(i)
+                graph.replay()
+                torch.cuda.synchronize()
+                for got, ref in zip(outs, refs[i]):
+                    assert torch.equal(got, ref), (rep, i)
+
+
+def test_pool_past_32_bit_offsets():
+    """Blocks whose bytes lie beyond 2^32 in the pool."""
+    L = _lib()
+    Hk, D = 8, 128
+    n = (1 << 32) // (Hk * 2 * 64 * D) + 40
+    codes, scales = L.readme_kv_cache(n, Hk, D, "cuda:0")
+    table = _i32([[n - 1, 3, n - 2]])
+    T = 150
+    k, v = (torch.randn(T, Hk * D, device="cuda:0").bfloat16() for _ in range(2))
+    q = torch.randn(T, Hk * D, device="cuda:0").bfloat16()
+    off, lens = _i32([0, T]), _i32([T])
+    L.readme_kv_write(1, k, v, off, lens, table, codes, scales)
+    o = L.readme_attention_kv(1, q, off, lens, table, codes, scales, H=Hk)
+    kb, vb = L.readme_kv_read(1, off, lens, table, codes, scales, T=T)
+    small = L.readme_kv_cache(4, Hk, D, "cuda:0")
+    t2 = _i32([[2, 0, 1]])
+    L.readme_kv_write(1, k, v, off, lens, t2, *small)
+    o2 = L.readme_attention_kv(1, q, off, lens, t2, *small, H=Hk)
+    kb2, vb2 = L.readme_kv_read(1, off, lens, t2, *small, T=T)
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2) and torch.equal(kb, kb2) and torch.equal(vb, vb2)
