@@ -145,4 +145,169 @@ __device__ __forceinline__ void row_keys(const KvAttnArgs& a, int len, int64_t p
     hi = (int)h;
 }
 
+// --- dealing the work out -------------------------------------------------------
+//
+// A pair is (request, tile of query rows, key head); its work is the blocks that
+// the request sees.  Either a workgroup takes a whole pair, or all blocks, pair
+// after pair (head fastest), are dealt to the workgroups in equal contiguous
+// shares, so that one long request among short ones, or few requests, fill the
+// chip alike.  A share may begin and end inside a pair: those ends are partial
+// results in the workspace, at most two per workgroup, which a second launch
+// joins (k_attention_join); a pair inside one share is written at once.
+
+struct KvPlan {
+    int64_t weight;  // blocks of all the request's pairs
+    int tiles;
+    int blocks;      // of each pair
+};
+
+template <int ROWS>
+__device__ __forceinline__ KvPlan kv_plan(const KvAttnArgs& a, const KvRequest& q) {
+    KvPlan p;
+    p.tiles = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
+    p.blocks = q.block1 - q.block0;
+    p.weight = (int64_t)p.tiles * a.c.Hk * p.blocks;
+    return p;
+}
+
+// Workspace: int64 [0] blocks per share, [1 + r] first block of request r's
+// pairs; then the parts, two per workgroup: sums [ROWS][D], m [ROWS], l [ROWS]
+// (fp32, sums in units of one).
+__host__ __device__ inline int64_t kv_plan_bytes(int64_t R) { return ((R + 1) * 8 + 255) / 256 * 256; }
+template <int D, int ROWS>
+constexpr int kv_part_floats = ROWS * (D + 2);
+
+__device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int64_t u = __shfl_up(v, off, 64);
+        if (lane >= off) v += u;
+    }
+    return v;
+}
+
+struct KvShare {
+    int64_t w0, w1;    // this workgroup's blocks
+    int64_t r, base;   // the request w0 lies in and that request's first block
+};
+
+// The workgroup's share; false if it has none.  Workgroup 0 writes the plan
+// down for the join.  `lds` holds WAVES + 2 int64.
+template <int ROWS, int WAVES>
+__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, int min_share, int64_t* plan,
+                                         int64_t* lds, KvShare& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int64_t R = a.c.R, grid = gridDim.x, me = blockIdx.x;
+    auto weight = [&](int64_t r) {
+        return r < R ? kv_plan<ROWS>(a, kv_request(a, r)).weight : (int64_t)0;
+    };
+    auto set = [&](int64_t total) {
+        int64_t share = (total + grid - 1) / grid;
+        share = share < min_share ? min_share : share;
+        sh.w0 = me * share;
+        sh.w1 = sh.w0 + share < total ? sh.w0 + share : total;
+        if (me == 0 && tid == 0) plan[0] = share;
+    };
+    if (R <= 64) {  // one request a lane, every wave for itself
+        const int64_t w = weight(lane), incl = wave_scan64(w, lane), base = incl - w;
+        const int64_t total = __shfl(incl, 63, 64);
+        set(total);
+        if (me == 0 && wv == 0 && lane < R) plan[1 + lane] = base;
+        if (sh.w0 >= total) return false;
+        const uint64_t at = __ballot(sh.w0 >= base && sh.w0 < base + w);
+        const int l = __ffsll((unsigned long long)at) - 1;
+        sh.r = l;
+        sh.base = __shfl(base, l, 64);
+        return true;
+    }
+    int64_t mine = 0;
+    for (int64_t r = tid; r < R; r += WAVES * 64) mine += weight(r);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) mine += __shfl_xor(mine, off, 64);
+    if (lane == 0) lds[wv] = mine;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += lds[w];
+    set(total);
+    if (sh.w0 >= total && me != 0) return false;
+    int64_t run = 0;
+    for (int64_t r0 = 0; r0 < R; r0 += WAVES * 64) {
+        const int64_t r = r0 + tid;
+        const int64_t w = weight(r), incl = wave_scan64(w, lane);
+        __syncthreads();
+        if (lane == 63) lds[wv] = incl;
+        __syncthreads();
+        int64_t base = run + incl - w;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            if (k < wv) base += lds[k];
+            run += lds[k];
+        }
+        if (sh.w0 >= base && sh.w0 < base + w) {
+            lds[WAVES] = r;
+            lds[WAVES + 1] = base;
+        }
+        if (me == 0 && r < R) plan[1 + r] = base;
+        if (me != 0 && run > sh.w0) break;
+    }
+    if (sh.w0 >= total) return false;
+    __syncthreads();
+    sh.r = lds[WAVES];
+    sh.base = lds[WAVES + 1];
+    return true;
+}
+
+// Tile j of request r is slot floor(offsets[r] G / ROWS) + r + j, which needs no
+// sum over the requests (and leaves some slots empty): the request of a slot,
+// and the tile.
+template <int ROWS>
+__device__ __forceinline__ int64_t kv_slot_request(const KvAttnArgs& a, int64_t slot, int64_t& tile) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, n = a.c.R;
+    while (n > 1) {
+        const int64_t step = (n + 63) / 64, i = lane * step;
+        const bool le = i < n && (int64_t)a.c.offsets[lo + i] * a.G / ROWS + lo + i <= slot;
+        const int below = __popcll(__ballot(le));
+        const int64_t skip = below > 0 ? (int64_t)(below - 1) * step : 0;
+        lo += skip;
+        n = n - skip < step ? n - skip : step;
+    }
+    tile = slot - ((int64_t)a.c.offsets[lo] * a.G / ROWS + lo);
+    return lo;
+}
+inline int64_t kv_slots(int64_t T, int64_t R, int64_t G, int rows) { return T * G / rows + R; }
+
+// One lane's block number and scales: block j of request r (-1: absent).
+struct KvBlockRef {
+    int blk;
+    float ks, vs;
+};
+__device__ __forceinline__ KvBlockRef kv_block_ref(const KvAttnArgs& a, int64_t r, int64_t j, int h) {
+    KvBlockRef b;
+    b.blk = (int)kv_block_of(a.c.table, a.c.max_blocks, a.c.n_blocks, r, j);
+    b.ks = b.vs = 0.0f;
+    if (b.blk >= 0) {
+        const float2 sc =
+            *reinterpret_cast<const float2*>(a.c.scales + ((int64_t)b.blk * a.c.Hk + h) * 2);
+        b.ks = sc.x;
+        b.vs = sc.y;
+    }
+    return b;
+}
+__device__ __forceinline__ KvBlockRef kv_lane_ref(const KvBlockRef& b, int lane) {
+    KvBlockRef o;
+    o.blk = __builtin_amdgcn_readlane(b.blk, lane);
+    o.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.ks), lane));
+    o.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.vs), lane));
+    return o;
+}
+
+constexpr int kRowsTile = 16;    // query rows of a pair in the two kernels
+constexpr int kTilesTile = 128;
+constexpr int kRowsShares = 1024;  // workgroups that shares are dealt to
+constexpr int kTilesShares = 512;
+hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s);
+hipError_t launch_attention_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
+
 }  // namespace readme

@@ -298,6 +298,19 @@ def test_attention(kt, D, Hk, G, case, causal, window):
     assert (got[sum(new):] == 55).all()
 
 
+@pytest.mark.parametrize("kt,D", [("i8", 64), ("e4m3", 128), ("i8", 256)])
+@pytest.mark.parametrize("window", [0, 70])
+def test_attention_many_pairs(kt, D, window):
+    """Enough requests that every workgroup takes a whole (rows, head) pair."""
+    rng = np.random.default_rng(50)
+    new = rng.integers(0, 10, 300)
+    lens = new + rng.integers(0, 100, 300)
+    c = _random_cache(kt, 300, 4, D, 2, seed=51)
+    c.table[7, 0] = -1
+    _poison_unused(c, lens)
+    _attend(c, list(new), list(lens), 16, window=window, pad=3)
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_attention_absent_blocks(new):
     """Blocks absent first, last, between and all: their tokens are not seen,
