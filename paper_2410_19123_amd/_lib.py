@@ -786,71 +786,89 @@ def readme_kv_scales_bytes(n_blocks: int, Hk: int) -> int:
     return int(load().readme_kv_scales_bytes(n_blocks, Hk))
 
 
-def _kv_rows(t, T: int, width: int, what: str) -> int:
-    """Row stride of rows [T][>= width] whose columns are contiguous."""
-    if not t.is_cuda:
-        raise ValueError("libreadme takes device tensors")
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != width or t.stride(1) != 1:
+def _kv_rows(t, T: int, width: int, dev: int, what: str) -> int:
+    """Row stride of rows [T][width] on device `dev` whose columns are
+    contiguous."""
+    if t.get_device() != dev:
+        raise ValueError(f"{what} must be on the cache's device")
+    stride = t.stride()
+    if t.shape != (T, width) or stride[1] != 1:
         raise ValueError(f"{what} must be [{T}][{width}] rows with contiguous columns")
-    return t.stride(0) if T > 1 else max(t.stride(0), width)
+    return stride[0] if T > 1 or stride[0] > width else width
 
 
 def _kv_cache_args(offsets, lens, table, codes, scales):
-    """(R, Hk, D, max_blocks, n_blocks) of a cache and the call's requests."""
-    _dev(offsets, lens, table, codes, scales)
-    for t, what in ((offsets, "offsets"), (lens, "lens"), (table, "table")):
-        if t.dtype != torch.int32:
-            raise ValueError(f"{what} must be int32")
-    if codes.dtype != torch.uint8 or codes.dim() != 4 or codes.shape[2] != 2 or \
-            codes.shape[3] % README_KV_BLOCK:
-        raise ValueError("codes must be uint8 [n_blocks][Hk][2][64 D]")
-    if scales.dtype != torch.float32 or scales.shape != codes.shape[:3]:
-        raise ValueError("scales must be fp32 [n_blocks][Hk][2]")
-    R = lens.shape[0]
-    if offsets.shape != (R + 1,) or lens.dim() != 1 or table.dim() != 2 or table.shape[0] != R:
-        raise ValueError("offsets [R+1], lens [R] and table [R][max_blocks] disagree")
-    return R, codes.shape[1], codes.shape[3] // README_KV_BLOCK, table.shape[1], codes.shape[0]
-
-
-def _kv_call(device, name: str, args, *tensors) -> None:
-    """The call on the device its tensors are on, which has to be one."""
-    for t in tensors:
-        if t.device != device:
+    """(R, Hk, D, max_blocks, n_blocks, device index) of a cache and the call's
+    requests.  One pass over the tensors: a step calls this once a layer."""
+    dev = codes.get_device()
+    if dev < 0:
+        raise ValueError("libreadme takes device tensors")
+    i32 = torch.int32
+    if offsets.dtype != i32 or lens.dtype != i32 or table.dtype != i32:
+        raise ValueError("offsets, lens and table must be int32")
+    if codes.dtype != torch.uint8 or scales.dtype != torch.float32:
+        raise ValueError("codes must be uint8 and scales fp32")
+    for t in (offsets, lens, table, codes, scales):
+        if t.get_device() != dev:
             raise ValueError("tensors on more than one device")
-    with torch.cuda.device(device):
-        _call(name, *args, _stream(device))
+        if not t.is_contiguous():
+            raise ValueError("libreadme takes contiguous tensors")
+    where, size = table.shape, codes.shape
+    if len(where) != 2 or offsets.shape != (where[0] + 1,) or lens.shape != (where[0],):
+        raise ValueError("offsets [R+1], lens [R] and table [R][max_blocks] disagree")
+    if len(size) != 4 or size[2] != 2 or size[3] % README_KV_BLOCK or scales.shape != size[:3]:
+        raise ValueError("codes must be [n_blocks][Hk][2][64 D] and scales [n_blocks][Hk][2]")
+    return where[0], size[1], size[3] // README_KV_BLOCK, where[1], size[0], dev
+
+
+# The current stream's handle without building a torch.cuda.Stream for it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _kv_call(dev: int, name: str, *args) -> None:
+    """The call on device `dev` (made current for it) and its current stream."""
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _kv_call(dev, name, *args)
+    st = getattr(load(), name)(*args, _raw_stream(dev) if _raw_stream is not None else
+                               torch.cuda.current_stream(dev).cuda_stream)
+    if st != 0:
+        raise ReadmeError(name, st)
 
 
 def readme_kv_write(kt: int, k, v, offsets, lens, table, codes, scales) -> None:
     """The call's rows k, v ([T][Hk D], bf16 or fp32; slices of wider rows
     allowed) into the cache, as 8-bit codes and one scale per block and head."""
-    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
     T = k.shape[0]
-    ld_k, ld_v = _kv_rows(k, T, Hk * D, "k"), _kv_rows(v, T, Hk * D, "v")
+    ld_k, ld_v = _kv_rows(k, T, Hk * D, dev, "k"), _kv_rows(v, T, Hk * D, dev, "v")
     if v.dtype != k.dtype:
         raise ValueError("k and v dtypes disagree")
-    _kv_call(codes.device, "readme_kv_write",
-             (kt, _dt(k), T, R, Hk, D, _p(k), ld_k, _p(v), ld_v, _p(offsets), _p(lens), _p(table),
-              mb, nb, _p(codes), _p(scales)), k, v, offsets, lens, table, scales)
+    _kv_call(dev, "readme_kv_write", kt, _dt(k), T, R, Hk, D, k.data_ptr(), ld_k, v.data_ptr(),
+             ld_v, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb,
+             codes.data_ptr(), scales.data_ptr())
 
 
 def readme_kv_read(kt: int, offsets, lens, table, codes, scales, k=None, v=None, T: int = None,
                    dtype=torch.bfloat16):
     """Cached rows back; returns (k, v) [T][Hk D].  Rows past offsets[R] keep
-    what they held."""
-    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    what they held.  T and dtype are those of k and v where given."""
+    R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
     if k is None or v is None:
-        rows = T if T is not None else (k if k is not None else v).shape[0]
-        dtype = k.dtype if k is not None else v.dtype if v is not None else dtype
-        k = k if k is not None else torch.empty((rows, Hk * D), dtype=dtype, device=codes.device)
-        v = v if v is not None else torch.empty((rows, Hk * D), dtype=dtype, device=codes.device)
+        given = k if k is not None else v
+        if given is not None:
+            T, dtype = given.shape[0], given.dtype
+        elif T is None:
+            raise ValueError("T, the number of rows, is needed where neither k nor v is given")
+        k = k if k is not None else torch.empty((T, Hk * D), dtype=dtype, device=codes.device)
+        v = v if v is not None else torch.empty((T, Hk * D), dtype=dtype, device=codes.device)
     T = k.shape[0]
-    ld_k, ld_v = _kv_rows(k, T, Hk * D, "k"), _kv_rows(v, T, Hk * D, "v")
+    ld_k, ld_v = _kv_rows(k, T, Hk * D, dev, "k"), _kv_rows(v, T, Hk * D, dev, "v")
     if v.dtype != k.dtype:
         raise ValueError("k and v dtypes disagree")
-    _kv_call(codes.device, "readme_kv_read",
-             (kt, _dt(k), T, R, Hk, D, _p(offsets), _p(lens), _p(table), mb, nb, _p(codes),
-              _p(scales), _p(k), ld_k, _p(v), ld_v), k, v, offsets, lens, table, scales)
+    _kv_call(dev, "readme_kv_read", kt, _dt(k), T, R, Hk, D, offsets.data_ptr(), lens.data_ptr(),
+             table.data_ptr(), mb, nb, codes.data_ptr(), scales.data_ptr(), k.data_ptr(), ld_k,
+             v.data_ptr(), ld_v)
     return k, v
 
 
@@ -863,23 +881,22 @@ def readme_attention_kv(kt: int, q, offsets, lens, table, codes, scales, H: int,
                         causal: bool = True, window: int = 0, o=None, workspace=None):
     """Attention of query rows q ([T][H D] bf16; slices of wider rows allowed)
     over the cache; scale defaults to 1 / sqrt(D).  Returns o [T][H D]."""
-    R, Hk, D, mb, nb = _kv_cache_args(offsets, lens, table, codes, scales)
+    R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
     T = q.shape[0]
-    if q.dtype != torch.bfloat16 or (o is not None and o.dtype != torch.bfloat16):
-        raise ValueError("q and o must be bf16")
     if o is None:
-        o = torch.empty((T, H * D), dtype=torch.bfloat16, device=q.device)
-    ld_q, ld_o = _kv_rows(q, T, H * D, "q"), _kv_rows(o, T, H * D, "o")
+        o = torch.empty((T, H * D), dtype=torch.bfloat16, device=codes.device)
+    if q.dtype != torch.bfloat16 or o.dtype != torch.bfloat16:
+        raise ValueError("q and o must be bf16")
+    ld_q, ld_o = _kv_rows(q, T, H * D, dev, "q"), _kv_rows(o, T, H * D, dev, "o")
     if workspace is None:
         ws = readme_attention_kv_workspace_bytes(T, R, H, Hk, D, mb)
-        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=q.device)
-    _dev(workspace)
-    scale = D ** -0.5 if scale is None else scale
-    _kv_call(codes.device, "readme_attention_kv",
-             (kt, T, R, H, Hk, D, _p(q), ld_q, _p(offsets), _p(lens), _p(table), mb, nb, _p(codes),
-              _p(scales), float(scale), int(bool(causal)), int(window), _p(o), ld_o, _p(workspace),
-              workspace.numel() * workspace.element_size()), q, o, offsets, lens, table, scales,
-             workspace)
+        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=codes.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous, on the cache's device")
+    _kv_call(dev, "readme_attention_kv", kt, T, R, H, Hk, D, q.data_ptr(), ld_q,
+             offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb, codes.data_ptr(),
+             scales.data_ptr(), D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+             o.data_ptr(), ld_o, workspace.data_ptr(), workspace.nbytes)
     return o
 
 

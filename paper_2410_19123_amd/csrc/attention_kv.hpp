@@ -84,15 +84,44 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2));
 }
 
-// A block's value scale against the running largest: log2 r and 1 / r.  Below
-// 2^-40 the block's values are under fp32's rounding of the rest and r stays
-// there; a NaN scale passes through the weights (a row that gives the block none
-// must not see it: 0 / r stays 0).
-__device__ __forceinline__ void value_ratio(float vs, float vref, float& log_r, float& inv_r) {
-    const float r = vs / vref;
-    const float c = r < 9.094947017729282e-13f ? 9.094947017729282e-13f : r;
-    log_r = __builtin_amdgcn_logf(c);
-    inv_r = c > 0.0f ? 1.0f / c : 1.0f;
+// Four fp32 to bf16, nearest even (the hardware conversion), 8 bytes.
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint2 pack_bf16(float a, float b, float c, float d) {
+    const f32x2v lo = {a, b}, hi = {c, d};
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2v)),
+                      __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2v)));
+}
+
+// A block's value scale against the running largest, log_vref = log2 vref:
+// log2 r and 1 / r.  Below 2^-40 the block's values are under fp32's rounding of
+// the rest and r stays there.
+__device__ __forceinline__ void value_ratio(float vs, float log_vref, float& log_r, float& inv_r) {
+    log_r = fmaxf(__builtin_amdgcn_logf(vs) - log_vref, -40.0f);
+    inv_r = __builtin_amdgcn_exp2f(-log_r);
+}
+
+// The scores' factor and offset of a row: 2^(factor * sum + offset) is a weight.
+// Both are finite and the factor positive, so that a masked sum of -infinity
+// gives 0 also in a row that has seen nothing (m = -infinity).
+__device__ __forceinline__ float score_factor(float cq, float ks) { return fmaxf(cq * ks, 1.2e-38f); }
+__device__ __forceinline__ float score_offset(float log_r, float m) {
+    return log_r + kUp - (m == -INFINITY ? 0.0f : m);
+}
+
+// A block whose scale is NaN: its weights become NaN where a row sees the token
+// and 0 elsewhere (v[k] is token k of the lane's, a row sees [a0, a1)).
+template <int N, class V>
+__device__ __forceinline__ void bad_weights(V& v, int a0, int a1, int first) {
+    asm volatile("");  // keeps this rare path a branch of its own
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        v[k] = first + k >= a0 && first + k < a1 ? __builtin_nanf("") : 0.0f;
+}
+template <int N, class V>
+__device__ __forceinline__ void mask_scores(V& v, int a0, int a1, int first) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        v[k] = (unsigned)(first + k - a0) < (unsigned)(a1 - a0) ? v[k] : -INFINITY;
 }
 
 // Query rows as fp16 matrix operands.  Each lane holds elements of one row in
@@ -148,17 +177,20 @@ __device__ __forceinline__ void row_keys(const KvAttnArgs& a, int len, int64_t p
 // --- dealing the work out -------------------------------------------------------
 //
 // A pair is (request, tile of query rows, key head); its work is the blocks that
-// the request sees.  Either a workgroup takes a whole pair, or all blocks, pair
-// after pair (head fastest), are dealt to the workgroups in equal contiguous
-// shares, so that one long request among short ones, or few requests, fill the
-// chip alike.  A share may begin and end inside a pair: those ends are partial
-// results in the workspace, at most two per workgroup, which a second launch
-// joins (k_attention_join); a pair inside one share is written at once.
+// the request sees.  Either a workgroup takes a whole pair, or all pairs, one
+// after the other (head fastest), are dealt to the workgroups in equal
+// contiguous shares, so that one long request among short ones, or few requests,
+// fill the chip alike.  A pair counts kPairCost units (its start and end) and one
+// for each block.  A share may begin and end inside a pair: those ends are
+// partial results in the workspace, at most two per workgroup, which a second
+// launch joins (k_attention_join); a pair whose blocks are all in one share is
+// written at once.
+constexpr int kPairCost = 6;
 
 struct KvPlan {
-    int64_t weight;  // blocks of all the request's pairs
+    int64_t weight;  // units of all the request's pairs
     int tiles;
-    int blocks;      // of each pair
+    int blocks;      // of each pair; a pair of none has no units
 };
 
 template <int ROWS>
@@ -166,13 +198,13 @@ __device__ __forceinline__ KvPlan kv_plan(const KvAttnArgs& a, const KvRequest& 
     KvPlan p;
     p.tiles = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
     p.blocks = q.block1 - q.block0;
-    p.weight = (int64_t)p.tiles * a.c.Hk * p.blocks;
+    p.weight = p.blocks > 0 ? (int64_t)p.tiles * a.c.Hk * (p.blocks + kPairCost) : 0;
     return p;
 }
 
-// Workspace: int64 [0] blocks per share, [1 + r] first block of request r's
-// pairs; then the parts, two per workgroup: sums [ROWS][D], m [ROWS], l [ROWS]
-// (fp32, sums in units of one).
+// Workspace: int64 [0] units per share, [1 + r] first unit of request r's pairs;
+// then the parts, two per workgroup: sums [ROWS][D], m [ROWS], l [ROWS] (fp32,
+// sums in units of one).
 __host__ __device__ inline int64_t kv_plan_bytes(int64_t R) { return ((R + 1) * 8 + 255) / 256 * 256; }
 template <int D, int ROWS>
 constexpr int kv_part_floats = ROWS * (D + 2);
@@ -186,77 +218,128 @@ __device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
     return v;
 }
 
-struct KvShare {
-    int64_t w0, w1;    // this workgroup's blocks
-    int64_t r, base;   // the request w0 lies in and that request's first block
-};
-
-// The workgroup's share; false if it has none.  Workgroup 0 writes the plan
-// down for the join.  `lds` holds WAVES + 2 int64.
+// A workgroup's way through its share, piece by piece.
 template <int ROWS, int WAVES>
-__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, int min_share, int64_t* plan,
-                                         int64_t* lds, KvShare& sh) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int64_t R = a.c.R, grid = gridDim.x, me = blockIdx.x;
-    auto weight = [&](int64_t r) {
-        return r < R ? kv_plan<ROWS>(a, kv_request(a, r)).weight : (int64_t)0;
-    };
-    auto set = [&](int64_t total) {
-        int64_t share = (total + grid - 1) / grid;
-        share = share < min_share ? min_share : share;
-        sh.w0 = me * share;
-        sh.w1 = sh.w0 + share < total ? sh.w0 + share : total;
-        if (me == 0 && tid == 0) plan[0] = share;
-    };
-    if (R <= 64) {  // one request a lane, every wave for itself
-        const int64_t w = weight(lane), incl = wave_scan64(w, lane), base = incl - w;
-        const int64_t total = __shfl(incl, 63, 64);
-        set(total);
-        if (me == 0 && wv == 0 && lane < R) plan[1 + lane] = base;
-        if (sh.w0 >= total) return false;
-        const uint64_t at = __ballot(sh.w0 >= base && sh.w0 < base + w);
-        const int l = __ffsll((unsigned long long)at) - 1;
-        sh.r = l;
-        sh.base = __shfl(base, l, 64);
+struct KvWalk {
+    int64_t w, w1;     // units left
+    int64_t base;      // first unit of request r
+    int64_t r, tile;
+    int h, b0, nb;     // blocks [b0, b0 + nb) of the pair's
+    KvRequest q;
+    KvPlan p;
+
+    // False if there is no share.  A share is at least `min_share` blocks, or a
+    // whole pair where the longest is shorter: cutting finer costs more in parts
+    // than it saves.  Workgroup 0 writes the plan down for the join.  `lds`
+    // holds 2 WAVES + 2 int64.
+    __device__ __forceinline__ bool start(const KvAttnArgs& a, int min_share, int64_t* plan,
+                                          int64_t* lds) {
+        const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+        const int64_t R = a.c.R, grid = gridDim.x, me = blockIdx.x;
+        int most = 0;  // blocks of the longest pair
+        auto weight = [&](int64_t at) {
+            if (at >= R) return (int64_t)0;
+            const KvPlan k = kv_plan<ROWS>(a, kv_request(a, at));
+            if (k.weight > 0) most = max(most, k.blocks);
+            return k.weight;
+        };
+        auto set = [&](int64_t total) {
+            int64_t share = (total + grid - 1) / grid;
+            const int64_t least = kPairCost + (most < min_share ? most : min_share);
+            share = share < least ? least : share;
+            w = me * share;
+            w1 = w + share < total ? w + share : total;
+            if (me == 0 && tid == 0) plan[0] = share;
+            return w < total;
+        };
+        auto wave_most = [&]() {
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) most = max(most, __shfl_xor(most, off, 64));
+        };
+        if (R <= 64) {  // one request a lane, every wave for itself
+            const int64_t v = weight(lane), incl = wave_scan64(v, lane), first = incl - v;
+            wave_most();
+            const bool any = set(__shfl(incl, 63, 64));
+            if (me == 0 && wv == 0 && lane < R) plan[1 + lane] = first;
+            if (!any) return false;
+            const int l = __ffsll((unsigned long long)__ballot(w >= first && w < incl)) - 1;
+            r = l;
+            base = __shfl(first, l, 64);
+        } else {
+            int64_t mine = 0;
+            for (int64_t i = tid; i < R; i += WAVES * 64) mine += weight(i);
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) mine += __shfl_xor(mine, off, 64);
+            wave_most();
+            if (lane == 0) {
+                lds[wv] = mine;
+                lds[WAVES + 2 + wv] = most;
+            }
+            __syncthreads();
+            int64_t total = 0;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                total += lds[k];
+                most = max(most, (int)lds[WAVES + 2 + k]);
+            }
+            const bool any = set(total);
+            if (!any && me != 0) return false;
+            int64_t run = 0;
+            for (int64_t r0 = 0; r0 < R; r0 += WAVES * 64) {
+                const int64_t i = r0 + tid;
+                const int64_t v = weight(i), incl = wave_scan64(v, lane);
+                __syncthreads();
+                if (lane == 63) lds[wv] = incl;
+                __syncthreads();
+                int64_t first = run + incl - v;
+#pragma unroll
+                for (int k = 0; k < WAVES; ++k) {
+                    if (k < wv) first += lds[k];
+                    run += lds[k];
+                }
+                if (w >= first && w < first + v) {
+                    lds[WAVES] = i;
+                    lds[WAVES + 1] = first;
+                }
+                if (me == 0 && i < R) plan[1 + i] = first;
+                if (me != 0 && run > w) break;
+            }
+            if (!any) return false;
+            __syncthreads();
+            r = lds[WAVES];
+            base = lds[WAVES + 1];
+        }
+        q = kv_request(a, r);
+        p = kv_plan<ROWS>(a, q);
         return true;
     }
-    int64_t mine = 0;
-    for (int64_t r = tid; r < R; r += WAVES * 64) mine += weight(r);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) mine += __shfl_xor(mine, off, 64);
-    if (lane == 0) lds[wv] = mine;
-    __syncthreads();
-    int64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) total += lds[w];
-    set(total);
-    if (sh.w0 >= total && me != 0) return false;
-    int64_t run = 0;
-    for (int64_t r0 = 0; r0 < R; r0 += WAVES * 64) {
-        const int64_t r = r0 + tid;
-        const int64_t w = weight(r), incl = wave_scan64(w, lane);
-        __syncthreads();
-        if (lane == 63) lds[wv] = incl;
-        __syncthreads();
-        int64_t base = run + incl - w;
-#pragma unroll
-        for (int k = 0; k < WAVES; ++k) {
-            if (k < wv) base += lds[k];
-            run += lds[k];
+
+    // The next piece with blocks; false at the share's end.
+    __device__ __forceinline__ bool next(const KvAttnArgs& a) {
+        while (w < w1) {
+            while (w >= base + p.weight) {  // ends: w is below the sum of all weights
+                base += p.weight;
+                q = kv_request(a, ++r);
+                p = kv_plan<ROWS>(a, q);
+            }
+            const int64_t units = p.blocks + kPairCost;
+            const int64_t pair = (w - base) / units;
+            const int u0 = (int)((w - base) - pair * units);
+            const int u1 = w1 - w < units - u0 ? u0 + (int)(w1 - w) : (int)units;
+            w += u1 - u0;
+            b0 = u0 > kPairCost ? u0 - kPairCost : 0;
+            nb = (u1 > kPairCost ? u1 - kPairCost : 0) - b0;
+            tile = pair / a.c.Hk;
+            h = (int)(pair - tile * a.c.Hk);
+            if (nb > 0) return true;
         }
-        if (sh.w0 >= base && sh.w0 < base + w) {
-            lds[WAVES] = r;
-            lds[WAVES + 1] = base;
-        }
-        if (me == 0 && r < R) plan[1 + r] = base;
-        if (me != 0 && run > sh.w0) break;
+        return false;
     }
-    if (sh.w0 >= total) return false;
-    __syncthreads();
-    sh.r = lds[WAVES];
-    sh.base = lds[WAVES + 1];
-    return true;
-}
+
+    __device__ __forceinline__ bool whole() const { return nb == p.blocks; }
+    // The pair begins in this share, or before it.
+    __device__ __forceinline__ int64_t part() const { return (int64_t)blockIdx.x * 2 + (b0 == 0 ? 1 : 0); }
+};
 
 // Tile j of request r is slot floor(offsets[r] G / ROWS) + r + j, which needs no
 // sum over the requests (and leaves some slots empty): the request of a slot,
@@ -303,11 +386,12 @@ __device__ __forceinline__ KvBlockRef kv_lane_ref(const KvBlockRef& b, int lane)
     return o;
 }
 
-constexpr int kRowsTile = 16;    // query rows of a pair in the two kernels
+constexpr int kRowsTile = 16;     // query rows of a pair, in the two kernels
 constexpr int kTilesTile = 128;
-constexpr int kRowsShares = 1024;  // workgroups that shares are dealt to
+constexpr int kRowsShares = 512;  // workgroups that shares are dealt to: two a CU
 constexpr int kTilesShares = 512;
-hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s);
+// `waves` of a workgroup that takes a whole pair (1, 2, 4, 8), or 0 for shares.
+hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attention_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
 
 }  // namespace readme

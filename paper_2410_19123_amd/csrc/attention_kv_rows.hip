@@ -1,13 +1,16 @@
 // Attention over the 8-bit cache for few query rows per request: decode steps
 // and drafted tokens (attention_kv.hpp has the mathematics).
 //
-//   The four waves of a workgroup take its blocks in turn, each straight from
-// global memory to registers with no LDS and no barrier:
-//     S^T = K Q^T   16x16x32 MFMA; a lane gets 16 scores of one row, the 16
+//   The waves of a workgroup take its blocks in turn, each straight from global
+// memory to registers with no LDS and no barrier:
+//     S^T = K Q^T   16x16x32 MFMA; a lane gets 16 scores of one row, of the 16
 //                   tokens whose codes it loads for V, so P stays in its
 //                   registers;
 //     O^T += V^T P^T.
-// The waves' sums meet in LDS at the end of a pair.
+// A block's K registers are loaded with the next block's codes as soon as the
+// scores have taken them, V's as soon as the sums have, so that 8 to 16 KB per
+// wave are always on their way.  The waves' sums meet in LDS at the end of a
+// pair.
 #include <math.h>
 
 #include "attention_kv.hpp"
@@ -16,344 +19,354 @@ namespace readme {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
-constexpr int kMinShare = 4;
+constexpr int kRows = kRowsTile;
+constexpr int kMinShare = 16;
 
-template <int D, int NT>
-constexpr int kXchgFloats = NT * (16 * D + 128);
-
-// One wave's running result over the blocks it takes.
-template <int KT, int D, int NT>
+// One wave's running result over the blocks it takes, for 16 rows.
+template <int KT, int D>
 struct RowsState {
-    f16x8 qf[NT][D / 32];
-    f32x4 acc[NT][D / 16];
-    float m[NT], l[NT], cq[NT];
-    int lo[NT], hi[NT];
-    float vref;
-    int min_hi, max_lo;
+    static constexpr int NK = D / 64;  // 16-byte pieces of K per lane and score tile
+    static constexpr int ND = D / 16;  // 16-dim tiles
+    f16x8 qf[2 * NK];
+    f32x4 acc[ND];
+    uint4 kf[4][NK], vf[ND];
+    float m, l, cq, vref, log_vref;
+    int lo, hi;          // keys this lane's row sees
+    int min_hi, max_lo;  // over the rows
 
-    __device__ __forceinline__ void start(const KvAttnArgs& a, const KvRequest& q, int tile, int h) {
+    // The lane's row of q, D / 4 elements of it; tok < 0 where there is none.
+    __device__ __forceinline__ void fetch(const KvAttnArgs& a, const KvRequest& q, int64_t tile, int h,
+                                          uint4 (&raw)[2 * NK], int& tok) {
         const int lane = threadIdx.x & 63, col = lane & 15, qt = lane >> 4;
-        min_hi = 0x7fffffff;
-        max_lo = 0;
-        vref = 0.0f;
+        const int64_t i = tile * kRows + col;
+        const bool real = i < (int64_t)q.n * a.G;
+        const int t = real ? (int)i / a.G : 0;  // i < n G <= 2^27
+        const int head = h * a.G + (real ? (int)i - t * a.G : 0);
+        const uint16_t* row = a.q + (q.row0 + t) * a.ld_q + (int64_t)head * D;
+        tok = real ? t : -1;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int i = (tile * NT + nt) * 16 + col;
-            const bool real = i < q.n * a.G;
-            const int tok = real ? i / a.G : 0;
-            const int head = h * a.G + (real ? i - tok * a.G : 0);
-            const uint16_t* row = a.q + (q.row0 + tok) * a.ld_q + (int64_t)head * D;
-            float x[D / 32][8];
-            float big = 0.0f;
-#pragma unroll
-            for (int f = 0; f < D / 32; ++f) {
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (real) w = *reinterpret_cast<const uint4*>(row + (f >> 1) * 64 + qt * 16 + (f & 1) * 8);
-                const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[f][2 * e] = bf16_lo(v[e]);
-                    x[f][2 * e + 1] = bf16_hi(v[e]);
-                    big = fmaxf(big, fmaxf(fabsf(x[f][2 * e]), fabsf(x[f][2 * e + 1])));
-                }
-            }
-            big = fmaxf(big, __shfl_xor(big, 16, 64));
-            big = fmaxf(big, __shfl_xor(big, 32, 64));
-            float up, down;
-            row_power(big, up, down);
-            cq[nt] = a.score * down;
-#pragma unroll
-            for (int f = 0; f < D / 32; ++f)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) qf[nt][f][e] = (_Float16)(x[f][e] * up);
-            row_keys(a, q.len, (int64_t)q.len - q.n + tok, lo[nt], hi[nt]);
-            if (real) {
-                min_hi = hi[nt] < min_hi ? hi[nt] : min_hi;
-                max_lo = lo[nt] > max_lo ? lo[nt] : max_lo;
-            }
-            m[nt] = -INFINITY;
-            l[nt] = 0.0f;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-                for (int i2 = 0; i2 < 4; ++i2) acc[nt][d][i2] = 0.0f;
-        }
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) {
-            const int u = __shfl_xor(min_hi, off, 64), w = __shfl_xor(max_lo, off, 64);
-            min_hi = u < min_hi ? u : min_hi;
-            max_lo = w > max_lo ? w : max_lo;
+        for (int f = 0; f < 2 * NK; ++f) {
+            raw[f] = make_uint4(0u, 0u, 0u, 0u);
+            if (real)
+                raw[f] =
+                    *reinterpret_cast<const uint4*>(row + (f >> 1) * 64 + qt * 16 + (f & 1) * 8);
         }
     }
 
-    // The 64 tokens of a block, token 0 at position j0.
-    __device__ __forceinline__ void block(const uint8_t* kc, float ks, float vs, int j0, int len) {
+    __device__ __forceinline__ void start(const KvAttnArgs& a, const KvRequest& q,
+                                          const uint4 (&raw)[2 * NK], int tok) {
+        min_hi = 0x7fffffff;
+        max_lo = 0;
+        float big = 0.0f;
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) {
+            const uint32_t v[4] = {raw[f].x, raw[f].y, raw[f].z, raw[f].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                big = fmaxf(big, fmaxf(fabsf(bf16_lo(v[e])), fabsf(bf16_hi(v[e]))));
+        }
+        big = fmaxf(big, __shfl_xor(big, 16, 64));
+        big = fmaxf(big, __shfl_xor(big, 32, 64));
+        float up, down;
+        row_power(big, up, down);
+        cq = a.score * down;
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) {
+            const uint32_t v[4] = {raw[f].x, raw[f].y, raw[f].z, raw[f].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                qf[f][2 * e] = (_Float16)(bf16_lo(v[e]) * up);
+                qf[f][2 * e + 1] = (_Float16)(bf16_hi(v[e]) * up);
+            }
+        }
+        const bool real = tok >= 0;
+        row_keys(a, q.len, (int64_t)q.len - q.n + (real ? tok : 0), lo, hi);
+        min_hi = real ? min(min_hi, hi) : min_hi;
+        max_lo = real ? max(max_lo, lo) : max_lo;
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) {
+            min_hi = min(min_hi, __shfl_xor(min_hi, off, 64));
+            max_lo = max(max_lo, __shfl_xor(max_lo, off, 64));
+        }
+        min_hi = __builtin_amdgcn_readfirstlane(min_hi);
+        max_lo = __builtin_amdgcn_readfirstlane(max_lo);
+    }
+
+    __device__ __forceinline__ void clear() {
+        vref = log_vref = 0.0f;
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    __device__ __forceinline__ void load_k(const uint8_t* kc) {
         const int lane = threadIdx.x & 63, col = lane & 15, qt = lane >> 4;
-        uint4 kf[4][D / 64], vf[D / 16];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int tok = 16 * (col >> 2) + 4 * t + (col & 3);
 #pragma unroll
-            for (int f = 0; f < D / 64; ++f)
+            for (int f = 0; f < NK; ++f)
                 kf[t][f] = *reinterpret_cast<const uint4*>(
                     kc + (((tok >> 5) * (D / 16) + 4 * f + qt) * 32 + (tok & 31)) * 16);
         }
+    }
+    __device__ __forceinline__ void load_v(const uint8_t* kc) {
+        const int lane = threadIdx.x & 63, col = lane & 15, qt = lane >> 4;
         const uint8_t* vc = kc + kKvBlock * D;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d)
+        for (int d = 0; d < ND; ++d)
             vf[d] = *reinterpret_cast<const uint4*>(vc + ((qt >> 1) * D + d * 16 + col) * 32 +
                                                     (qt & 1) * 16);
-        if (j0 + kKvBlock > len) {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) vf[d] = keep_tokens(vf[d], len - j0 - 16 * qt);
-        }
+    }
 
-        f32x4 s[NT][4];
+    // The block held in kf and vf, its token 0 at position j0; `next` is the
+    // block whose codes take its place.
+    __device__ __forceinline__ void block(float ks, float vs, int j0, int len, const uint8_t* next) {
+        const int qt = (threadIdx.x & 63) >> 4;
+        f32x4 s[4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int t = 0; t < 4; ++t) {
+            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int t = 0; t < 4; ++t) s[nt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int f = 0; f < D / 64; ++f) {
+            for (int f = 0; f < NK; ++f) {
                 const f16x8 k0 = cvt8<KT>(kf[t][f].x, kf[t][f].y);
                 const f16x8 k1 = cvt8<KT>(kf[t][f].z, kf[t][f].w);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    s[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[nt][2 * f], s[nt][t], 0, 0, 0);
-                    s[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[nt][2 * f + 1], s[nt][t], 0, 0, 0);
-                }
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[2 * f], s[t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[2 * f + 1], s[t], 0, 0, 0);
             }
+        }
+        load_k(next);
 
         // Units of the sums: the largest value scale so far.
         if (vs > vref) {
-            const float f = vref / vs;
+            const float f = vref * __builtin_amdgcn_rcpf(vs);
             vref = vs;
+            log_vref = __builtin_amdgcn_logf(vs);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int d = 0; d < D / 16; ++d) acc[nt][d] *= f;
+            for (int d = 0; d < ND; ++d) acc[d] *= f;
         }
         float log_r, inv_r;
-        value_ratio(vs, vref, log_r, inv_r);
+        value_ratio(vs, log_vref, log_r, inv_r);
 
-        const bool masked = j0 + kKvBlock > min_hi || j0 < max_lo;
-        f16x8 pf[NT][2];
+        const float c = score_factor(cq, ks);
+        // score k = 4 t + i of the lane is token j0 + 16 qt + k
+        float z[16];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float c = cq[nt] * ks;
-            // score (t, i) is token j0 + 16 qt + 4 t + i
-            const int a0 = lo[nt] - j0 - 16 * qt, a1 = hi[nt] - j0 - 16 * qt;
-            float mx = -INFINITY;
+        for (int k = 0; k < 16; ++k) z[k] = s[k >> 2][k & 3];
+        const int a0 = lo - j0 - 16 * qt, a1 = hi - j0 - 16 * qt;
+        if (j0 + kKvBlock > min_hi || j0 < max_lo) mask_scores<16>(z, a0, a1, 0);
+        float mx = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+        for (int k = 0; k < 16; ++k) mx = fmaxf(mx, z[k]);
+        if (__any(mx * c > m + kLazy)) {
+            float t = mx * c;
+            t = fmaxf(t, __shfl_xor(t, 16, 64));
+            t = fmaxf(t, __shfl_xor(t, 32, 64));
+            const float mn = fmaxf(m, t);
+            const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (masked && (4 * t + i < a0 || 4 * t + i >= a1)) s[nt][t][i] = -INFINITY;
-                    mx = fmaxf(mx, s[nt][t][i]);
-                }
-            if (__any(mx * c > m[nt] + kLazy)) {
-                float t = mx * c;
-                t = fmaxf(t, __shfl_xor(t, 16, 64));
-                t = fmaxf(t, __shfl_xor(t, 32, 64));
-                const float mn = fmaxf(m[nt], t);
-                const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-                m[nt] = mn;
-                l[nt] *= f;
+            for (int d = 0; d < ND; ++d) acc[d] *= f;
+        }
+        const float b = score_offset(log_r, m);
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) acc[nt][d] *= f;
-            }
-            const float b = log_r + kUp - m[nt];
-            float sum = 0.0f;
-            uint32_t pw[8];
+        for (int k = 0; k < 16; ++k) z[k] = __builtin_amdgcn_exp2f(fmaf(z[k], c, b));
+        if (!(ks < INFINITY && vs < INFINITY)) bad_weights<16>(z, a0, a1, 0);
+        float sum = 0.0f;
+        f16x8 pf[2];
+        uint32_t pw[8];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float p[4];
+        for (int i = 0; i < 16; i += 2) {
+            sum += z[i];
+            sum += z[i + 1];
+            pw[i / 2] = pack_f16(z[i], z[i + 1]);
+        }
+        l = fmaf(sum, inv_r, l);
+        pf[0] = __builtin_bit_cast(f16x8, u32x4v{pw[0], pw[1], pw[2], pw[3]});
+        pf[1] = __builtin_bit_cast(f16x8, u32x4v{pw[4], pw[5], pw[6], pw[7]});
+        if (j0 + kKvBlock > len) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(s[nt][t][i], c, b));
-                    if (masked && (4 * t + i < a0 || 4 * t + i >= a1)) p[i] = 0.0f;
-                    sum += p[i];
-                }
-                pw[2 * t] = pack_f16(p[0], p[1]);
-                pw[2 * t + 1] = pack_f16(p[2], p[3]);
-            }
-            l[nt] = fmaf(sum, inv_r, l[nt]);
-            pf[nt][0] = __builtin_bit_cast(f16x8, u32x4v{pw[0], pw[1], pw[2], pw[3]});
-            pf[nt][1] = __builtin_bit_cast(f16x8, u32x4v{pw[4], pw[5], pw[6], pw[7]});
+            for (int d = 0; d < ND; ++d) vf[d] = keep_tokens(vf[d], len - j0 - 16 * qt);
         }
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
+        for (int d = 0; d < ND; ++d) {
             const f16x8 v0 = cvt8<KT>(vf[d].x, vf[d].y);
             const f16x8 v1 = cvt8<KT>(vf[d].z, vf[d].w);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                acc[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[nt][0], acc[nt][d], 0, 0, 0);
-                acc[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[nt][1], acc[nt][d], 0, 0, 0);
-            }
+            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[0], acc[d], 0, 0, 0);
+            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[1], acc[d], 0, 0, 0);
         }
+        load_v(next);
     }
 
-    // l over the whole row, sums in units of one.
-    __device__ __forceinline__ void finish() {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            l[nt] += __shfl_xor(l[nt], 16, 64);
-            l[nt] += __shfl_xor(l[nt], 32, 64);
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) acc[nt][d] *= vref;
-        }
-    }
-
-    // In LDS, between the waves: sums [NT][D / 16][64 lanes] float4, then m and l
-    // [NT][2][64 lanes].
-    __device__ __forceinline__ void put(float* part) const {
+    // Blocks first, first + stride, ... below nb of the request's blocks from b0
+    // on.
+    __device__ __forceinline__ void walk(const KvAttnArgs& a, const KvRequest& q, int64_t tile, int64_t r,
+                                         int h, int b0, int nb, int first, int stride) {
         const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-                reinterpret_cast<f32x4*>(part)[(nt * (D / 16) + d) * 64 + lane] = acc[nt][d];
-            float* ml = part + NT * 16 * D + nt * 128;
-            ml[lane] = m[nt];
-            ml[64 + lane] = l[nt];
-        }
-    }
-    __device__ __forceinline__ void join(const float* part) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float* ml = part + NT * 16 * D + nt * 128;
-            const float m1 = ml[lane], l1 = ml[64 + lane];
-            const float mn = fmaxf(m[nt], m1);
-            const float base = mn == -INFINITY ? 0.0f : mn;
-            const float f0 = __builtin_amdgcn_exp2f(m[nt] - base);
-            const float f1 = __builtin_amdgcn_exp2f(m1 - base);
-            m[nt] = mn;
-            l[nt] = l[nt] * f0 + l1 * f1;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-                acc[nt][d] = acc[nt][d] * f0 +
-                             reinterpret_cast<const f32x4*>(part)[(nt * (D / 16) + d) * 64 + lane] * f1;
-        }
-    }
-
-    // The rows in bf16 where they belong.
-    __device__ __forceinline__ void store(const KvAttnArgs& a, const KvRequest& q, int tile, int h) const {
-        const int lane = threadIdx.x & 63, col = lane & 15, qt = lane >> 4;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int i = (tile * NT + nt) * 16 + col;
-            if (i >= q.n * a.G) continue;
-            const int tok = i / a.G, head = h * a.G + i - tok * a.G;
-            uint16_t* row = a.o + (q.row0 + tok) * a.ld_o + (int64_t)head * D + 4 * qt;
-            const float inv = l[nt] == 0.0f ? 0.0f : 1.0f / l[nt];
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-                uint2 w;
-                w.x = (uint32_t)f32_to_bf16(acc[nt][d][0] * inv) | ((uint32_t)f32_to_bf16(acc[nt][d][1] * inv) << 16);
-                w.y = (uint32_t)f32_to_bf16(acc[nt][d][2] * inv) | ((uint32_t)f32_to_bf16(acc[nt][d][3] * inv) << 16);
-                *reinterpret_cast<uint2*>(row + d * 16) = w;
+        uint4 raw[2 * NK];
+        int tok;
+        fetch(a, q, tile, h, raw, tok);
+        clear();
+        // Lane i holds the number and scales of the wave's i-th of the current
+        // 64 blocks; absent blocks are stepped over.
+        KvBlockRef refs;
+        const int cnt = first < nb ? (nb - first + stride - 1) / stride : 0;
+        auto next = [&](int i, KvBlockRef& b) {
+            for (; i < cnt; ++i) {
+                if ((i & 63) == 0) {
+                    refs.blk = -1;
+                    refs.ks = refs.vs = 0.0f;
+                    if (i + lane < cnt) refs = kv_block_ref(a, r, b0 + first + (i + lane) * stride, h);
+                }
+                b = kv_lane_ref(refs, i & 63);
+                if (b.blk >= 0) break;
             }
+            return i;
+        };
+        auto codes = [&](int blk) {
+            return a.c.codes + ((int64_t)blk * a.c.Hk + h) * 2 * kKvBlock * D;
+        };
+        KvBlockRef cur, nxt;
+        int i = next(0, cur);
+        if (i < cnt) {
+            load_k(codes(cur.blk));
+            load_v(codes(cur.blk));
         }
-    }
-    __device__ __forceinline__ void store_part(float* part) const {
-        const int lane = threadIdx.x & 63, col = lane & 15, qt = lane >> 4;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int i = nt * 16 + col;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-                *reinterpret_cast<f32x4*>(part + i * D + d * 16 + 4 * qt) = acc[nt][d];
-            if (qt == 0) {
-                part[16 * NT * D + i] = m[nt];
-                part[16 * NT * (D + 1) + i] = l[nt];
-            }
+        start(a, q, raw, tok);
+        while (i < cnt) {
+            nxt = cur;
+            const int in = next(i + 1, nxt);
+            // Past the last block the loads repeat it (cached, and in bounds).
+            const int to = in < cnt ? nxt.blk : cur.blk;
+            block(cur.ks, cur.vs, (b0 + first + i * stride) * kKvBlock, q.len, codes(to));
+            i = in;
+            cur = nxt;
         }
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] *= vref;
     }
 };
 
-template <int KT, int D, int NT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
-void k_attention_rows(KvAttnArgs a, int64_t* __restrict__ plan, float* __restrict__ parts) {
-    constexpr int kRows = 16 * NT;
-    __shared__ __attribute__((aligned(16))) float xs[2 * kXchgFloats<D, NT>];
-    __shared__ int64_t found[kWaves + 2];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    KvShare sh;
-    if (!kv_share<kRows, kWaves>(a, kMinShare, plan, found, sh)) return;
+// LDS of W waves: sums [wave][D / 16][64 lanes] float4, then m and l
+// [wave][16 rows].
+template <int D, int W>
+constexpr int kXchgFloats = W * kRows * (D + 2);
 
-    int64_t r = sh.r, base = sh.base;
-    KvRequest q = kv_request(a, r);
-    KvPlan p = kv_plan<kRows>(a, q);
-    RowsState<KT, D, NT> st;
-    for (int64_t w = sh.w0; w < sh.w1;) {
-        while (w >= base + p.weight) {  // ends: w is below the sum of all weights
-            base += p.weight;
-            q = kv_request(a, ++r);
-            p = kv_plan<kRows>(a, q);
+// Joins the waves' sums; each wave's 16-dim tiles of a row go to o, or to `part`
+// before the division by l.
+template <int KT, int D, int W>
+__device__ __forceinline__ void join_waves(const KvAttnArgs& a, const KvRequest& q, int64_t tile, int h,
+                                           const RowsState<KT, D>& st, float* xs, float* part) {
+    constexpr int ND = D / 16;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, col = lane & 15;
+    float* xm = xs + W * kRows * D;
+    float* xl = xm + W * kRows;
+    __syncthreads();  // an earlier pair's reads are over
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+        reinterpret_cast<f32x4*>(xs)[(wv * ND + d) * 64 + lane] = st.acc[d];
+    if (lane < kRows) {
+        xm[wv * kRows + col] = st.m;
+        xl[wv * kRows + col] = st.l;
+    }
+    __syncthreads();
+        float f[W], mx = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) mx = fmaxf(mx, xm[w * kRows + col]);
+    const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(xm[w * kRows + col] - base);
+        l = fmaf(xl[w * kRows + col], f[w], l);
+    }
+    const int64_t i = tile * kRows + col;
+    const bool real = i < (int64_t)q.n * a.G;
+    const int tok = real ? (int)i / a.G : 0, head = h * a.G + (real ? (int)i - tok * a.G : 0);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int d0 = 0; d0 < ND; d0 += W) {
+        const int d = d0 + wv;
+        if (d >= ND) break;
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            s += reinterpret_cast<const f32x4*>(xs)[(w * ND + d) * 64 + lane] * f[w];
+        const int at = d * 16 + 4 * (lane >> 4);
+        if (part) {
+            *reinterpret_cast<f32x4*>(part + col * D + at) = s;
+        } else if (real) {
+            *reinterpret_cast<uint2*>(a.o + (q.row0 + tok) * a.ld_o + (int64_t)head * D + at) =
+                pack_bf16(s[0] * inv, s[1] * inv, s[2] * inv, s[3] * inv);
         }
-        const int pair = (int)((w - base) / p.blocks);
-        const int b0 = (int)((w - base) - (int64_t)pair * p.blocks);
-        const int left = p.blocks - b0;
-        const int nb = sh.w1 - w < left ? (int)(sh.w1 - w) : left;
-        const int tile = pair / a.c.Hk, h = pair - tile * a.c.Hk;
-        st.start(a, q, tile, h);
-        // Wave wv takes blocks wv, wv + 4, ...; lane i holds the block number
-        // and scales of the wave's i-th of the next 64.
-        for (int i0 = wv; i0 < nb; i0 += 64 * kWaves) {
-            KvBlockRef mine;
-            mine.blk = -1;
-            if (i0 + lane * kWaves < nb)
-                mine = kv_block_ref(a, r, q.block0 + b0 + i0 + lane * kWaves, h);
-            const int cnt = (nb - i0 + kWaves - 1) / kWaves;
-            for (int k = 0; k < (cnt < 64 ? cnt : 64); ++k) {
-                const KvBlockRef b = kv_lane_ref(mine, k);
-                if (b.blk < 0) continue;
-                st.block(a.c.codes + ((int64_t)b.blk * a.c.Hk + h) * 2 * kKvBlock * D, b.ks, b.vs,
-                         (q.block0 + b0 + i0 + k * kWaves) * kKvBlock, q.len);
-            }
-        }
-        st.finish();
-        // Waves 2 and 3 into 0 and 1, then 1 into 0.
-        __syncthreads();
-        if (wv >= 2) st.put(xs + (wv - 2) * kXchgFloats<D, NT>);
-        __syncthreads();
-        if (wv < 2) st.join(xs + wv * kXchgFloats<D, NT>);
-        __syncthreads();
-        if (wv == 1) st.put(xs);
-        __syncthreads();
-        if (wv == 0) {
-            st.join(xs);
-            if (nb == p.blocks)
-                st.store(a, q, tile, h);
-            else
-                st.store_part(parts + ((int64_t)blockIdx.x * 2 + (b0 == 0 ? 1 : 0)) *
-                                          kv_part_floats<D, kRows>);
-        }
-        w += nb;
+    }
+    if (part && threadIdx.x < kRows) {
+        part[kRows * D + col] = mx;
+        part[kRows * (D + 1) + col] = l;
     }
 }
 
+template <int KT, int D, int W, bool SHARES>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2)))
+void k_attention_rows(KvAttnArgs a, int64_t* __restrict__ plan, float* __restrict__ parts) {
+    __shared__ __attribute__((aligned(16))) float xs[kXchgFloats<D, W>];
+    const int wv = threadIdx.x >> 6;
+    RowsState<KT, D> st;
+    if constexpr (!SHARES) {
+        int64_t tile;
+        const int h = (int)(blockIdx.x % a.c.Hk);
+        const int64_t r = kv_slot_request<kRows>(a, blockIdx.x / a.c.Hk, tile);
+        const KvRequest q = kv_request(a, r);
+        if (tile < 0 || tile * kRows >= (int64_t)q.n * a.G) return;
+        st.walk(a, q, tile, r, h, q.block0, q.block1 - q.block0, wv, W);
+        join_waves<KT, D, W>(a, q, tile, h, st, xs, nullptr);
+    } else {
+        __shared__ int64_t found[2 * W + 2];
+        KvWalk<kRows, W> wk;
+        if (!wk.start(a, kMinShare, plan, found)) return;
+        while (wk.next(a)) {
+            st.walk(a, wk.q, wk.tile, wk.r, wk.h, wk.q.block0 + wk.b0, wk.nb, wv, W);
+            join_waves<KT, D, W>(a, wk.q, wk.tile, wk.h, st, xs,
+                                 wk.whole() ? nullptr : parts + wk.part() * kv_part_floats<D, kRows>);
+        }
+    }
+}
+
+template <int KT, int D, int W>
+void whole(const KvAttnArgs& a, hipStream_t s) {
+    const int64_t grid = kv_slots(a.c.T, a.c.R, a.G, kRows) * a.c.Hk;
+    k_attention_rows<KT, D, W, false><<<(unsigned)grid, W * 64, 0, s>>>(a, nullptr, nullptr);
+}
+
 template <int KT, int D>
-hipError_t rows_of(const KvAttnArgs& a, hipStream_t s) {
-    int64_t* plan = reinterpret_cast<int64_t*>(a.ws);
-    float* parts = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kv_plan_bytes(a.c.R));
-    k_attention_rows<KT, D, 1><<<kRowsShares, kThreads, 0, s>>>(a, plan, parts);
+hipError_t rows_of(const KvAttnArgs& a, int waves, hipStream_t s) {
+    if (waves == 0) {
+        int64_t* plan = reinterpret_cast<int64_t*>(a.ws);
+        float* parts = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kv_plan_bytes(a.c.R));
+        k_attention_rows<KT, D, 4, true><<<kRowsShares, 256, 0, s>>>(a, plan, parts);
+    } else if (waves == 1) {
+        whole<KT, D, 1>(a, s);
+    } else if (waves == 2) {
+        whole<KT, D, 2>(a, s);
+    } else if (waves == 4 || D == 256) {
+        whole<KT, D, 4>(a, s);
+    } else {
+        if constexpr (D < 256) whole<KT, D, 8>(a, s);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {
+hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s) {
     const bool i8 = kt == README_KV_I8;
     switch (a.c.D) {
-        case 64: return i8 ? rows_of<README_KV_I8, 64>(a, s) : rows_of<README_KV_E4M3, 64>(a, s);
-        case 128: return i8 ? rows_of<README_KV_I8, 128>(a, s) : rows_of<README_KV_E4M3, 128>(a, s);
-        case 256: return i8 ? rows_of<README_KV_I8, 256>(a, s) : rows_of<README_KV_E4M3, 256>(a, s);
+        case 64: return i8 ? rows_of<README_KV_I8, 64>(a, waves, s) : rows_of<README_KV_E4M3, 64>(a, waves, s);
+        case 128: return i8 ? rows_of<README_KV_I8, 128>(a, waves, s) : rows_of<README_KV_E4M3, 128>(a, waves, s);
+        case 256: return i8 ? rows_of<README_KV_I8, 256>(a, waves, s) : rows_of<README_KV_E4M3, 256>(a, waves, s);
     }
     return hipErrorInvalidValue;
 }

@@ -30,7 +30,7 @@ struct TileState {
     static constexpr int ND = D / 32;
     f16x8 qf[NQ];
     f32x16 acc[ND];
-    float m, l, cq, vref;
+    float m, l, cq, vref, log_vref;
     int lo, hi;                  // keys this lane's row sees
     int min_hi, max_hi, min_lo, max_lo;  // over the wave's rows
     bool real;                   // the lane's row exists
@@ -90,7 +90,7 @@ struct TileState {
         max_lo = __builtin_amdgcn_readfirstlane(max_lo);
         m = -INFINITY;
         l = 0.0f;
-        vref = 0.0f;
+        vref = log_vref = 0.0f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -113,25 +113,26 @@ struct TileState {
             }
         }
         if (vs > vref) {
-            const float f = vref / vs;
+            const float f = vref * __builtin_amdgcn_rcpf(vs);
             vref = vs;
+            log_vref = __builtin_amdgcn_logf(vs);
 #pragma unroll
             for (int d = 0; d < ND; ++d) acc[d] *= f;
         }
         float log_r, inv_r;
-        value_ratio(vs, vref, log_r, inv_r);
-        const float c = cq * ks;
-        const bool masked = j0 + kKvBlock > min_hi || j0 < max_lo;
+        value_ratio(vs, log_vref, log_r, inv_r);
+        const float c = score_factor(cq, ks);
         // score (g, k) is token j0 + 32 g + 16 hf + k
         const int a0 = lo - j0 - 16 * hf, a1 = hi - j0 - 16 * hf;
+        if (j0 + kKvBlock > min_hi || j0 < max_lo) {
+            mask_scores<16>(s[0], a0, a1, 0);
+            mask_scores<16>(s[1], a0, a1, 32);
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                if (masked && (32 * g + k < a0 || 32 * g + k >= a1)) s[g][k] = -INFINITY;
-                mx = fmaxf(mx, s[g][k]);
-            }
+            for (int k = 0; k < 16; ++k) mx = fmaxf(mx, s[g][k]);
         if (__any(mx * c > m + kLazy)) {
             float t = mx * c;
             t = fmaxf(t, __shfl_xor(t, 32, 64));
@@ -142,27 +143,28 @@ struct TileState {
 #pragma unroll
             for (int d = 0; d < ND; ++d) acc[d] *= f;
         }
-        const float b = log_r + kUp - m;
+        const float b = score_offset(log_r, m);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s[g][k] = __builtin_amdgcn_exp2f(fmaf(s[g][k], c, b));
+        if (!(ks < INFINITY && vs < INFINITY)) {
+            bad_weights<16>(s[0], a0, a1, 0);
+            bad_weights<16>(s[1], a0, a1, 32);
+        }
         float sum = 0.0f;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            uint32_t pw[8];
-#pragma unroll
-            for (int k = 0; k < 16; k += 2) {
-                float p0 = __builtin_amdgcn_exp2f(fmaf(s[g][k], c, b));
-                float p1 = __builtin_amdgcn_exp2f(fmaf(s[g][k + 1], c, b));
-                if (masked) {
-                    if (32 * g + k < a0 || 32 * g + k >= a1) p0 = 0.0f;
-                    if (32 * g + k + 1 < a0 || 32 * g + k + 1 >= a1) p1 = 0.0f;
-                }
-                sum += p0;
-                sum += p1;
-                pw[k / 2] = pack_f16(p0, p1);
-            }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const f16x8 pf = __builtin_bit_cast(
-                    f16x8, u32x4v{pw[4 * st], pw[4 * st + 1], pw[4 * st + 2], pw[4 * st + 3]});
+                u32x4v pw;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    sum += s[g][8 * st + 2 * k];
+                    sum += s[g][8 * st + 2 * k + 1];
+                    pw[k] = pack_f16(s[g][8 * st + 2 * k], s[g][8 * st + 2 * k + 1]);
+                }
+                const f16x8 pf = __builtin_bit_cast(f16x8, pw);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
                     const f16x8 vf =
@@ -184,12 +186,10 @@ struct TileState {
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint2 w;
-                w.x = (uint32_t)f32_to_bf16(acc[d][4 * g] * inv) | ((uint32_t)f32_to_bf16(acc[d][4 * g + 1] * inv) << 16);
-                w.y = (uint32_t)f32_to_bf16(acc[d][4 * g + 2] * inv) | ((uint32_t)f32_to_bf16(acc[d][4 * g + 3] * inv) << 16);
-                *reinterpret_cast<uint2*>(row + d * 32 + 8 * g) = w;
-            }
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<uint2*>(row + d * 32 + 8 * g) =
+                    pack_bf16(acc[d][4 * g] * inv, acc[d][4 * g + 1] * inv, acc[d][4 * g + 2] * inv,
+                              acc[d][4 * g + 3] * inv);
     }
     __device__ __forceinline__ void store_part(float* part) const {
         const int lane = threadIdx.x & 63, i = (threadIdx.x >> 6) * 32 + (lane & 31), hf = lane >> 5;
@@ -321,33 +321,17 @@ void k_attention_tiles(KvAttnArgs a, int64_t* __restrict__ plan, float* __restri
         st.finish();
         st.store(a);
     } else {
-        __shared__ int64_t found[kWaves + 2];
-        KvShare sh;
-        if (!kv_share<kTilesTile, kWaves>(a, kMinShare, plan, found, sh)) return;
-        int64_t r = sh.r, base = sh.base;
-        KvRequest q = kv_request(a, r);
-        KvPlan p = kv_plan<kTilesTile>(a, q);
-        for (int64_t w = sh.w0; w < sh.w1;) {
-            while (w >= base + p.weight) {  // ends: w is below the sum of all weights
-                base += p.weight;
-                q = kv_request(a, ++r);
-                p = kv_plan<kTilesTile>(a, q);
-            }
-            const int64_t pair = (w - base) / p.blocks;
-            const int b0 = (int)((w - base) - pair * p.blocks);
-            const int left = p.blocks - b0;
-            const int nb = sh.w1 - w < left ? (int)(sh.w1 - w) : left;
-            const int64_t tile = pair / a.c.Hk;
-            const int h = (int)(pair - tile * a.c.Hk);
-            st.start(a, q, tile, h);
-            walk<KT, D>(a, q, r, h, q.block0 + b0, nb, lds, st);
+        __shared__ int64_t found[2 * kWaves + 2];
+        KvWalk<kTilesTile, kWaves> wk;
+        if (!wk.start(a, kMinShare, plan, found)) return;
+        while (wk.next(a)) {
+            st.start(a, wk.q, wk.tile, wk.h);
+            walk<KT, D>(a, wk.q, wk.r, wk.h, wk.q.block0 + wk.b0, wk.nb, lds, st);
             st.finish();
-            if (nb == p.blocks)
+            if (wk.whole())
                 st.store(a);
             else
-                st.store_part(parts + ((int64_t)blockIdx.x * 2 + (b0 == 0 ? 1 : 0)) *
-                                          kv_part_floats<D, kTilesTile>);
-            w += nb;
+                st.store_part(parts + wk.part() * kv_part_floats<D, kTilesTile>);
         }
     }
 }

@@ -299,6 +299,26 @@ def test_attention(kt, D, Hk, G, case, causal, window):
 
 
 @pytest.mark.parametrize("kt,D", [("i8", 64), ("e4m3", 128), ("i8", 256)])
+@pytest.mark.parametrize("new,G,max_blocks", [
+    ([1, 1, 1], 4, 3), ([1] * 40, 4, 3), ([1] * 90, 2, 3), ([1] * 150, 2, 3),  # 8, 4, 2, 1 waves
+    ([1, 2, 1], 4, 100), ([1] * 70, 2, 80),                                    # shares of rows
+    ([60, 1, 70], 3, 90), ([40] * 3 + [0] * 70, 3, 90),                        # shares of tiles
+    ([80] * 30, 4, 6), ([80] * 12, 4, 12),                                     # tiles, whole pairs
+])
+def test_attention_every_form(kt, D, new, G, max_blocks):
+    """The launch shapes the sizes choose, one by one: requests of 0 .. 190
+    tokens (a table as wide as max_blocks says)."""
+    rng = np.random.default_rng(len(new) + max_blocks)
+    lens = [n + int(x) for n, x in zip(new, rng.integers(0, 110, len(new)))]
+    c = _random_cache(kt, len(new), 3, D, 3, seed=60)
+    wide = np.full((len(new), max_blocks), -1, np.int32)
+    wide[:, :3] = c.table
+    c.table = wide
+    _poison_unused(c, lens)
+    _attend(c, new, lens, 3 * G, pad=1)
+
+
+@pytest.mark.parametrize("kt,D", [("i8", 64), ("e4m3", 128), ("i8", 256)])
 @pytest.mark.parametrize("window", [0, 70])
 def test_attention_many_pairs(kt, D, window):
     """Enough requests that every workgroup takes a whole (rows, head) pair."""
