@@ -18,7 +18,7 @@
 // is either the first of its request in this call (one candidate per request)
 // or begins at one of the call's rows; a request has at most one such row in a
 // run of 64, so a workgroup per run of 64 rows finds them.  Both kernels run
-// one wave per (candidate, head, K or V) and need no plan and no workspace.
+// one workgroup per (candidate, head, K or V) and need no plan and no workspace.
 #include <math.h>
 
 #include "kv_cache.hpp"
@@ -29,38 +29,40 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// 16 consecutive values of a row in fp32.
+// 16 consecutive values of a row, as they are stored.
 template <int DT>
-__device__ __forceinline__ void load16(const void* base, int64_t at, float (&x)[16]) {
-    if constexpr (DT == README_BF16) {
-        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + at);
-        const uint4 a = p[0], b = p[1];
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+struct Row16 {
+    uint4 v[DT == README_BF16 ? 2 : 4];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[2 * i] = bf16_lo(w[i]);
-            x[2 * i + 1] = bf16_hi(w[i]);
-        }
-    } else {
-        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 a = p[i];
-            x[4 * i] = a.x;
-            x[4 * i + 1] = a.y;
-            x[4 * i + 2] = a.z;
-            x[4 * i + 3] = a.w;
-        }
+        for (auto& x : v) x = make_uint4(0u, 0u, 0u, 0u);
     }
-}
+    __device__ __forceinline__ void load(const void* base, int64_t at) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(base) +
+                                                        at * (DT == README_BF16 ? 2 : 4));
+#pragma unroll
+        for (auto& x : v) x = *p++;
+    }
+    __device__ __forceinline__ float at(int k) const {
+        const int d = DT == README_BF16 ? k >> 1 : k;
+        const uint4 q = v[d >> 2];
+        const uint32_t w = (d & 3) == 0 ? q.x : (d & 3) == 1 ? q.y : (d & 3) == 2 ? q.z : q.w;
+        if constexpr (DT == README_F32) return __uint_as_float(w);
+        return k & 1 ? bf16_hi(w) : bf16_lo(w);
+    }
+};
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <int DT>
 __device__ __forceinline__ void store16(void* base, int64_t at, const float (&x)[16]) {
     if constexpr (DT == README_BF16) {
         uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
+        for (int i = 0; i < 8; ++i) {  // the hardware conversion, nearest even
+            const f32x2 p = {x[2 * i], x[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+        }
         uint4* p = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + at);
         p[0] = make_uint4(w[0], w[1], w[2], w[3]);
         p[1] = make_uint4(w[4], w[5], w[6], w[7]);
@@ -105,13 +107,22 @@ __device__ __forceinline__ uint32_t encode(float x, float s, float inv) {
     }
 }
 
-// The value a code stands for, and the code nearest to a value on the grid's
-// own scale (ties to even).
+// Four codes times s.
 template <int KT>
-__device__ __forceinline__ float decode(uint32_t b) {
-    if constexpr (KT == README_KV_I8) return (float)((int)b - 128);
-    return __builtin_amdgcn_cvt_f32_fp8((int)b, 0);
+__device__ __forceinline__ void decode4(uint32_t w, float s, float* x) {
+    if constexpr (KT == README_KV_I8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (float)((int)((w >> (8 * e)) & 0xffu) - 128) * s;
+    } else {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+        const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        x[0] = a[0] * s;
+        x[1] = a[1] * s;
+        x[2] = b[0] * s;
+        x[3] = b[1] * s;
+    }
 }
+// The code nearest to a code's value times f (ties to even).
 template <int KT>
 __device__ __forceinline__ uint32_t regrid(uint32_t b, float f) {
     if constexpr (KT == README_KV_I8) return (uint32_t)((int)rintf((float)((int)b - 128) * f) + 128);
@@ -186,40 +197,76 @@ __device__ __forceinline__ void for_touched(const KvCacheArgs& c, int64_t cand, 
     }
 }
 
-// LDS bytes of one V wave: 64 token rows of D codes, four bytes apart per row
-// so that a column's bytes spread over the banks.
-constexpr int kv_lds_row(int D) { return D + 4; }
+constexpr int kThreads = 256;
+// LDS holds a block's V codes as 64 token rows, one dword apart so that a
+// column's dwords spread over the banks.
+constexpr int kv_lds_row(int D) { return D / 4 + 1; }
 
-// One wave's block of K (half 0) or V (half 1).
+// Four dwords of four bytes each, transposed: byte j of out[i] is byte i of
+// in[j].
+__device__ __forceinline__ void transpose4(const uint32_t (&in)[4], uint32_t (&out)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(in[1], in[0], 0x05010400u);  // 0.0 1.0 0.1 1.1
+    const uint32_t b = __builtin_amdgcn_perm(in[1], in[0], 0x07030602u);  // 0.2 1.2 0.3 1.3
+    const uint32_t c = __builtin_amdgcn_perm(in[3], in[2], 0x05010400u);
+    const uint32_t d = __builtin_amdgcn_perm(in[3], in[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// A thread's part of a V block in memory: eight tokens t0 .. t0 + 7 of four
+// dims d0 .. d0 + 3, as two dwords a dim.  Item i of 2 D; four neighbours make
+// a dim's 32 bytes.
+struct VPiece {
+    int t0, d0;
+};
+__device__ __forceinline__ VPiece v_piece(int D, int i) {
+    VPiece p;
+    p.t0 = (i / D) * 32 + (i & 3) * 8;
+    p.d0 = (i % D >> 2) * 4;
+    return p;
+}
+
+// One block of K or V, by the whole workgroup: a thread holds 16 values of a
+// row per pass, the rows stay in registers between the maximum and the codes.
 template <int KT, int DT, int D, bool V>
 __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched& b, int h,
-                                            const void* src, int64_t ld, uint8_t* lds) {
+                                            const void* src, int64_t ld, uint32_t* lds,
+                                            uint32_t* most) {
     const int64_t blk = kv_block_of(c.table, c.max_blocks, c.n_blocks, b.r, b.j);
     if (blk < 0) return;
-    const int lane = threadIdx.x & 63;
-    constexpr int LPR = D / 16;      // lanes per row, 16 values each
-    constexpr int RPP = 64 / LPR;    // rows per pass
-    const int ch = lane % LPR, rw = lane / LPR;
+    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int LPR = D / 16;           // threads per row
+    constexpr int RPP = kThreads / LPR;   // rows per pass
+    constexpr int NP = kKvBlock / RPP;
+    const int ch = tid % LPR, rw = tid / LPR;
     const int64_t unit = (blk * c.Hk + h) * 2 + (V ? 1 : 0);
     uint8_t* dst = c.codes + unit * kv_half_bytes(D);
     const int64_t col = (int64_t)h * D + ch * 16;
+    const float old = b.slot > 0 ? c.scales[unit] : 1.0f;
 
+    Row16<DT> x[NP];
     uint32_t am = 0;
-    for (int i = rw; i < b.n; i += RPP) {
-        float x[16];
-        load16<DT>(src, (b.tok + i) * ld + col, x);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const uint32_t u = __float_as_uint(x[k]) & 0x7fffffffu;
-            am = u > am ? u : am;
-        }
+    for (int p = 0; p < NP; ++p) {
+        x[p].zero();
+        if (p * RPP + rw < b.n) x[p].load(src, (b.tok + p * RPP + rw) * ld + col);
     }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) am = max(am, __float_as_uint(x[p].at(k)) & 0x7fffffffu);
     am = wave_max_u32(am);
+    __syncthreads();  // an earlier block's reads of `most` and `lds` are over
+    if (lane == 0) most[tid >> 6] = am;
+    __syncthreads();
+    am = max(max(most[0], most[1]), max(most[2], most[3]));
+
     const float need = __uint_as_float(am) / kv_qmax<KT>();
     float s = fmaxf(need, kKvScaleFloor), shrink = 1.0f;
     bool bad = am >= 0x7f800000u;
     if (b.slot > 0) {
-        const float old = c.scales[unit];
         int e_need, e_old;
         (void)frexpf(need, &e_need);
         const float m = frexpf(old, &e_old);
@@ -235,13 +282,12 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
         shrink = 1.0f;
     }
     const bool grown = shrink != 1.0f;
-    if (lane == 0) c.scales[unit] = s;
+    if (tid == 0) c.scales[unit] = s;
     const float inv = 1.0f / s;
-    const uint32_t zero = KT == README_KV_I8 ? 0x80808080u : 0u;
 
     if constexpr (!V) {
         if (grown) {
-            for (int i = lane; i < b.slot * LPR; i += 64) {
+            for (int i = tid; i < b.slot * LPR; i += kThreads) {
                 uint4* p = reinterpret_cast<uint4*>(dst + kv_k_byte(D, i / LPR, (i % LPR) * 16));
                 uint4 w = *p;
                 w.x = regrid4<KT>(w.x, shrink);
@@ -252,26 +298,27 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
             }
         }
     }
-    const bool staged = V && (grown || b.n > RPP);
-    for (int i = rw; i < b.n; i += RPP) {
-        uint32_t w[4] = {zero, zero, zero, zero};
-        if (!bad) {
-            float x[16];
-            load16<DT>(src, (b.tok + i) * ld + col, x);
+    // Few rows of V go byte by byte, more (and a block whose earlier codes
+    // change) through LDS.
+    const bool staged = V && (grown || b.n > 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                w[k] = 0;
+    for (int p = 0; p < NP; ++p) {
+        const int i = p * RPP + rw;
+        if (i >= b.n) break;
+        uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[k] |= encode<KT>(x[4 * k + e], s, inv) << (8 * e);
-            }
+        for (int k = 0; k < 4; ++k) {
+            w[k] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[k] |= encode<KT>(x[p].at(4 * k + e), s, inv) << (8 * e);
+            if (bad) w[k] = KT == README_KV_I8 ? 0x80808080u : 0u;
         }
         if constexpr (!V) {
             *reinterpret_cast<uint4*>(dst + kv_k_byte(D, b.slot + i, ch * 16)) =
                 make_uint4(w[0], w[1], w[2], w[3]);
         } else if (staged) {
-            uint32_t* row = reinterpret_cast<uint32_t*>(lds + (b.slot + i) * kv_lds_row(D) + ch * 16);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) row[k] = w[k];
+            for (int k = 0; k < 4; ++k) lds[(b.slot + i) * kv_lds_row(D) + ch * 4 + k] = w[k];
         } else {
 #pragma unroll
             for (int k = 0; k < 16; ++k)
@@ -280,115 +327,145 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
     }
     if constexpr (V) {
         if (!staged) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        // 16 tokens of one dim at a time: the new bytes from LDS, the earlier
-        // ones rescaled, later ones left as they were.
+        __syncthreads();
         const int end = b.slot + b.n;
-        for (int i = lane; i < 4 * D; i += 64) {
-            const int d = i >> 1 & (D - 1), t0 = (i / (2 * D)) * 32 + (i & 1) * 16;
-            if (t0 >= end || (t0 + 16 <= b.slot && !grown)) continue;
-            uint4* p = reinterpret_cast<uint4*>(dst + kv_v_byte(D, t0, d));
-            uint4 old = make_uint4(0u, 0u, 0u, 0u);
-            if (t0 < b.slot || t0 + 16 > end) old = *p;
-            uint32_t w[4] = {old.x, old.y, old.z, old.w};
+        for (int i = tid; i < 2 * D; i += kThreads) {
+            const VPiece v = v_piece(D, i);
+            if (v.t0 >= end || (v.t0 + 8 <= b.slot && !grown)) continue;
+            uint32_t in[2][4], out[2][4];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int t = t0 + k, sh = 8 * (k & 3);
-                uint32_t byte = (w[k >> 2] >> sh) & 0xffu;
-                if (t >= b.slot && t < end) byte = lds[t * kv_lds_row(D) + d];
-                else if (t < b.slot && grown) byte = regrid<KT>(byte, shrink);
-                w[k >> 2] = (w[k >> 2] & ~(0xffu << sh)) | (byte << sh);
+            for (int e = 0; e < 8; ++e) in[e >> 2][e & 3] = lds[(v.t0 + e) * kv_lds_row(D) + v.d0 / 4];
+            transpose4(in[0], out[0]);
+            transpose4(in[1], out[1]);
+            uint8_t* at = dst + kv_v_byte(D, v.t0, v.d0);
+            if (v.t0 >= b.slot && v.t0 + 8 <= end) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    *reinterpret_cast<uint2*>(at + 32 * k) = make_uint2(out[0][k], out[1][k]);
+            } else {
+                // Earlier tokens keep their (rescaled) codes, later bytes theirs.
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint2 was = *reinterpret_cast<const uint2*>(at + 32 * k);
+                    uint32_t w[2] = {was.x, was.y};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int t = v.t0 + e, sh = 8 * (e & 3);
+                        uint32_t byte = (w[e >> 2] >> sh) & 0xffu;
+                        if (t >= b.slot && t < end) byte = (out[e >> 2][k] >> sh) & 0xffu;
+                        else if (t < b.slot && grown) byte = regrid<KT>(byte, shrink);
+                        w[e >> 2] = (w[e >> 2] & ~(0xffu << sh)) | (byte << sh);
+                    }
+                    *reinterpret_cast<uint2*>(at + 32 * k) = make_uint2(w[0], w[1]);
+                }
             }
-            *p = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        // The next block of this wave writes the same LDS rows.
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
-// Two waves: K and V of (candidate blockIdx.x, head blockIdx.y).
+// K (blockIdx.z = 0) or V of (candidate blockIdx.x, head blockIdx.y).
 template <int KT, int DT, int D>
-__global__ __launch_bounds__(128) void k_kv_write(KvCacheArgs c, const void* __restrict__ k,
-                                                  int64_t ld_k, const void* __restrict__ v,
-                                                  int64_t ld_v) {
-    __shared__ uint8_t lds[kKvBlock * kv_lds_row(D)];
+__global__ __launch_bounds__(kThreads) void k_kv_write(KvCacheArgs c, const void* __restrict__ k,
+                                                       int64_t ld_k, const void* __restrict__ v,
+                                                       int64_t ld_v) {
+    __shared__ uint32_t lds[kKvBlock * kv_lds_row(D)];
+    __shared__ uint32_t most[4];
     const int h = blockIdx.y;
-    const bool isv = threadIdx.x >= 64;
-    for_touched(c, blockIdx.x, [&](const Touched& b) {
-        if (isv) write_block<KT, DT, D, true>(c, b, h, v, ld_v, lds);
-        else write_block<KT, DT, D, false>(c, b, h, k, ld_k, lds);
-    });
+    if (blockIdx.z)
+        for_touched(c, blockIdx.x, [&](const Touched& b) {
+            write_block<KT, DT, D, true>(c, b, h, v, ld_v, lds, most);
+        });
+    else
+        for_touched(c, blockIdx.x, [&](const Touched& b) {
+            write_block<KT, DT, D, false>(c, b, h, k, ld_k, lds, most);
+        });
 }
 
 template <int KT, int DT, int D, bool V>
 __device__ __forceinline__ void read_block(const KvCacheArgs& c, const Touched& b, int h, void* out,
-                                           int64_t ld, uint8_t* lds) {
-    const int lane = threadIdx.x & 63;
-    constexpr int LPR = D / 16, RPP = 64 / LPR;
-    const int ch = lane % LPR, rw = lane / LPR;
+                                           int64_t ld, uint32_t* lds) {
+    const int tid = threadIdx.x;
+    constexpr int LPR = D / 16, RPP = kThreads / LPR, NP = kKvBlock / RPP;
+    const int ch = tid % LPR, rw = tid / LPR;
     const int64_t blk = kv_block_of(c.table, c.max_blocks, c.n_blocks, b.r, b.j);
     const int64_t unit = blk < 0 ? 0 : (blk * c.Hk + h) * 2 + (V ? 1 : 0);
     const uint8_t* src = c.codes + unit * kv_half_bytes(D);
     const float s = blk < 0 ? 0.0f : c.scales[unit];
     const int64_t col = (int64_t)h * D + ch * 16;
+    uint32_t w[NP][4];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[p][k] = KT == README_KV_I8 ? 0x80808080u : 0u;
     if constexpr (V) {
         if (blk >= 0) {
-            for (int i = lane; i < 4 * D; i += 64) {
-                const int d = i >> 1 & (D - 1), t0 = (i / (2 * D)) * 32 + (i & 1) * 16;
-                if (t0 >= b.slot + b.n || t0 + 16 <= b.slot) continue;
-                const uint4 w = *reinterpret_cast<const uint4*>(src + kv_v_byte(D, t0, d));
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+            constexpr int NI = 2 * D / kThreads > 0 ? 2 * D / kThreads : 1;
+            uint32_t in[NI][2][4];
 #pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    lds[(t0 + k) * kv_lds_row(D) + d] = (uint8_t)(ws[k >> 2] >> (8 * (k & 3)));
+            for (int j = 0; j < NI; ++j) {
+                const int i = tid + j * kThreads;
+                if (i >= 2 * D) break;
+                const VPiece v = v_piece(D, i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint2 a = *reinterpret_cast<const uint2*>(src + kv_v_byte(D, v.t0, v.d0 + k));
+                    in[j][0][k] = a.x;
+                    in[j][1][k] = a.y;
+                }
             }
+            __syncthreads();  // an earlier block's reads are over
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int i = tid + j * kThreads;
+                if (i >= 2 * D) break;
+                const VPiece v = v_piece(D, i);
+                uint32_t o[4];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    transpose4(in[j][q], o);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) lds[(v.t0 + 4 * q + e) * kv_lds_row(D) + v.d0 / 4] = o[e];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+                if (p * RPP + rw < b.n)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        w[p][k] = lds[(b.slot + p * RPP + rw) * kv_lds_row(D) + ch * 4 + k];
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+    } else if (blk >= 0) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            if (p * RPP + rw < b.n) {
+                const uint4 a = *reinterpret_cast<const uint4*>(
+                    src + kv_k_byte(D, b.slot + p * RPP + rw, ch * 16));
+                w[p][0] = a.x;
+                w[p][1] = a.y;
+                w[p][2] = a.z;
+                w[p][3] = a.w;
+            }
     }
-    for (int i = rw; i < b.n; i += RPP) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        if (p * RPP + rw >= b.n) break;
         float x[16];
-        if (blk < 0) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) x[k] = 0.0f;
-        } else {
-            uint32_t w[4];
-            if constexpr (V) {
-                const uint32_t* row =
-                    reinterpret_cast<const uint32_t*>(lds + (b.slot + i) * kv_lds_row(D) + ch * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = row[k];
-            } else {
-                const uint4 a =
-                    *reinterpret_cast<const uint4*>(src + kv_k_byte(D, b.slot + i, ch * 16));
-                w[0] = a.x;
-                w[1] = a.y;
-                w[2] = a.z;
-                w[3] = a.w;
-            }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) x[k] = decode<KT>((w[k >> 2] >> (8 * (k & 3))) & 0xffu) * s;
-        }
-        store16<DT>(out, (b.tok + i) * ld + col, x);
-    }
-    if constexpr (V) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        for (int k = 0; k < 4; ++k) decode4<KT>(w[p][k], s, &x[4 * k]);
+        store16<DT>(out, (b.tok + p * RPP + rw) * ld + col, x);
     }
 }
 
 template <int KT, int DT, int D>
-__global__ __launch_bounds__(128) void k_kv_read(KvCacheArgs c, void* __restrict__ k, int64_t ld_k,
-                                                 void* __restrict__ v, int64_t ld_v) {
-    __shared__ uint8_t lds[kKvBlock * kv_lds_row(D)];
+__global__ __launch_bounds__(kThreads) void k_kv_read(KvCacheArgs c, void* __restrict__ k, int64_t ld_k,
+                                                      void* __restrict__ v, int64_t ld_v) {
+    __shared__ uint32_t lds[kKvBlock * kv_lds_row(D)];
     const int h = blockIdx.y;
-    const bool isv = threadIdx.x >= 64;
-    for_touched(c, blockIdx.x, [&](const Touched& b) {
-        if (isv) read_block<KT, DT, D, true>(c, b, h, v, ld_v, lds);
-        else read_block<KT, DT, D, false>(c, b, h, k, ld_k, lds);
-    });
+    if (blockIdx.z)
+        for_touched(c, blockIdx.x, [&](const Touched& b) { read_block<KT, DT, D, true>(c, b, h, v, ld_v, lds); });
+    else
+        for_touched(c, blockIdx.x, [&](const Touched& b) { read_block<KT, DT, D, false>(c, b, h, k, ld_k, lds); });
 }
 
 template <template <int, int, int> class L, class... A>
@@ -412,14 +489,14 @@ hipError_t by_type(readme_kv_type kt, readme_dtype dt, int D, A... a) {
 }
 
 dim3 kv_grid(const KvCacheArgs& c) {
-    return dim3((unsigned)(c.R + ceil_div(c.T, kKvBlock)), (unsigned)c.Hk);
+    return dim3((unsigned)(c.R + ceil_div(c.T, kKvBlock)), (unsigned)c.Hk, 2u);
 }
 
 template <int KT, int DT, int D>
 struct WriteOp {
     static hipError_t go(KvCacheArgs c, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                          hipStream_t s) {
-        k_kv_write<KT, DT, D><<<kv_grid(c), 128, 0, s>>>(c, k, ld_k, v, ld_v);
+        k_kv_write<KT, DT, D><<<kv_grid(c), kThreads, 0, s>>>(c, k, ld_k, v, ld_v);
         return hipGetLastError();
     }
 };
@@ -427,7 +504,7 @@ template <int KT, int DT, int D>
 struct ReadOp {
     static hipError_t go(KvCacheArgs c, void* k, int64_t ld_k, void* v, int64_t ld_v,
                          hipStream_t s) {
-        k_kv_read<KT, DT, D><<<kv_grid(c), 128, 0, s>>>(c, k, ld_k, v, ld_v);
+        k_kv_read<KT, DT, D><<<kv_grid(c), kThreads, 0, s>>>(c, k, ld_k, v, ld_v);
         return hipGetLastError();
     }
 };
