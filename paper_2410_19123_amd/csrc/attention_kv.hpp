@@ -108,20 +108,20 @@ __device__ __forceinline__ float score_offset(float log_r, float m) {
     return log_r + kUp - (m == -INFINITY ? 0.0f : m);
 }
 
-// A block whose scale is NaN: its weights become NaN where a row sees the token
-// and 0 elsewhere (v[k] is token k of the lane's, a row sees [a0, a1)).
-template <int N, class V>
-__device__ __forceinline__ void bad_weights(V& v, int a0, int a1, int first) {
-    asm volatile("");  // keeps this rare path a branch of its own
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-        v[k] = first + k >= a0 && first + k < a1 ? __builtin_nanf("") : 0.0f;
+// A block whose key or value scale is not finite: every row that sees any of its
+// tokens becomes NaN through its sum (the factor and offset above stay finite, so
+// other rows' weights for it are 0).
+__device__ __forceinline__ bool bad_scales(float ks, float vs) { return !(ks < INFINITY && vs < INFINITY); }
+__device__ __forceinline__ float bad_sum(float l, int lo, int hi, int j0) {
+    return max(lo, j0) < min(hi, j0 + kKvBlock) ? __builtin_nanf("") : l;
 }
-template <int N, class V>
-__device__ __forceinline__ void mask_scores(V& v, int a0, int a1, int first) {
+
+// Token k of a lane's 16 is seen if a0 <= k < a1.
+template <class V>
+__device__ __forceinline__ void mask_scores(V& v, int a0, int a1) {
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-        v[k] = (unsigned)(first + k - a0) < (unsigned)(a1 - a0) ? v[k] : -INFINITY;
+    for (int k = 0; k < 16; ++k)
+        v[k] = (unsigned)(k - a0) < (unsigned)(a1 - a0) ? v[k] : -INFINITY;
 }
 
 // Query rows as fp16 matrix operands.  Each lane holds elements of one row in
@@ -218,6 +218,13 @@ __device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
     return v;
 }
 
+// A value that is the same in all lanes, to scalar registers.
+__device__ __forceinline__ int64_t wave_uniform(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
 // A workgroup's way through its share, piece by piece.
 template <int ROWS, int WAVES>
 struct KvWalk {
@@ -247,6 +254,8 @@ struct KvWalk {
             int64_t share = (total + grid - 1) / grid;
             const int64_t least = kPairCost + (most < min_share ? most : min_share);
             share = share < least ? least : share;
+            share = wave_uniform(share);
+            total = wave_uniform(total);
             w = me * share;
             w1 = w + share < total ? w + share : total;
             if (me == 0 && tid == 0) plan[0] = share;
@@ -264,7 +273,7 @@ struct KvWalk {
             if (!any) return false;
             const int l = __ffsll((unsigned long long)__ballot(w >= first && w < incl)) - 1;
             r = l;
-            base = __shfl(first, l, 64);
+            base = wave_uniform(__shfl(first, l, 64));
         } else {
             int64_t mine = 0;
             for (int64_t i = tid; i < R; i += WAVES * 64) mine += weight(i);
@@ -306,8 +315,8 @@ struct KvWalk {
             }
             if (!any) return false;
             __syncthreads();
-            r = lds[WAVES];
-            base = lds[WAVES + 1];
+            r = wave_uniform(lds[WAVES]);
+            base = wave_uniform(lds[WAVES + 1]);
         }
         q = kv_request(a, r);
         p = kv_plan<ROWS>(a, q);
@@ -359,7 +368,7 @@ __device__ __forceinline__ int64_t kv_slot_request(const KvAttnArgs& a, int64_t 
     tile = slot - ((int64_t)a.c.offsets[lo] * a.G / ROWS + lo);
     return lo;
 }
-inline int64_t kv_slots(int64_t T, int64_t R, int64_t G, int rows) { return T * G / rows + R; }
+__host__ __device__ inline int64_t kv_slots(int64_t T, int64_t R, int64_t G, int rows) { return T * G / rows + R; }
 
 // One lane's block number and scales: block j of request r (-1: absent).
 struct KvBlockRef {

@@ -155,7 +155,7 @@ struct RowsState {
 #pragma unroll
         for (int k = 0; k < 16; ++k) z[k] = s[k >> 2][k & 3];
         const int a0 = lo - j0 - 16 * qt, a1 = hi - j0 - 16 * qt;
-        if (j0 + kKvBlock > min_hi || j0 < max_lo) mask_scores<16>(z, a0, a1, 0);
+        if (j0 + kKvBlock > min_hi || j0 < max_lo) mask_scores(z, a0, a1);
         float mx = -INFINITY;
 #pragma unroll
         for (int k = 0; k < 16; ++k) mx = fmaxf(mx, z[k]);
@@ -173,7 +173,6 @@ struct RowsState {
         const float b = score_offset(log_r, m);
 #pragma unroll
         for (int k = 0; k < 16; ++k) z[k] = __builtin_amdgcn_exp2f(fmaf(z[k], c, b));
-        if (!(ks < INFINITY && vs < INFINITY)) bad_weights<16>(z, a0, a1, 0);
         float sum = 0.0f;
         f16x8 pf[2];
         uint32_t pw[8];
@@ -184,6 +183,7 @@ struct RowsState {
             pw[i / 2] = pack_f16(z[i], z[i + 1]);
         }
         l = fmaf(sum, inv_r, l);
+        if (bad_scales(ks, vs)) l = bad_sum(l, lo, hi, j0);
         pf[0] = __builtin_bit_cast(f16x8, u32x4v{pw[0], pw[1], pw[2], pw[3]});
         pf[1] = __builtin_bit_cast(f16x8, u32x4v{pw[4], pw[5], pw[6], pw[7]});
         if (j0 + kKvBlock > len) {
@@ -219,6 +219,9 @@ struct RowsState {
                     refs.blk = -1;
                     refs.ks = refs.vs = 0.0f;
                     if (i + lane < cnt) refs = kv_block_ref(a, r, b0 + first + (i + lane) * stride, h);
+                    // Wait for them here, not wherever the paths meet again (which
+                    // would wait for every code on its way as well).
+                    asm volatile("" : "+v"(refs.blk), "+v"(refs.ks), "+v"(refs.vs));
                 }
                 b = kv_lane_ref(refs, i & 63);
                 if (b.blk >= 0) break;

@@ -23,6 +23,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kMinShare = 8;
+constexpr int kSchedMfma = 0x8, kSchedRead = 0x100;  // __builtin_amdgcn_sched_group_barrier
 
 template <int KT, int D>
 struct TileState {
@@ -101,17 +102,39 @@ struct TileState {
     __device__ __forceinline__ void block(const uint8_t* kl, const uint8_t* vl, float ks, float vs, int j0) {
         if (j0 >= max_hi || j0 + kKvBlock <= min_lo) return;
         const int lane = threadIdx.x & 63, hf = lane >> 5;
+        // Operands are read kAhead steps before their product, so that an LDS
+        // round trip hides behind other products (4 and 6: the same time, and
+        // registers spilled where shares are dealt).
+        constexpr int kAhead = 2;
+        auto k_at = [&](int i) {  // step i: token half i % 2, dims i / 2
+            return *reinterpret_cast<const f16x8*>(kl + (((i & 1) * NQ + (i >> 1)) * 64 + lane) * 16);
+        };
+        auto v_at = [&](int i) {
+            return *reinterpret_cast<const f16x8*>(vl + (i * 64 + lane) * 16);
+        };
         f32x16 s[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int k = 0; k < 16; ++k) s[g][k] = 0.0f;
+        {
+            f16x8 f[2 * NQ];
 #pragma unroll
-            for (int u = 0; u < NQ; ++u) {
-                const f16x8 kf = *reinterpret_cast<const f16x8*>(kl + ((g * NQ + u) * 64 + lane) * 16);
-                s[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[u], s[g], 0, 0, 0);
+            for (int i = 0; i < 2 * NQ; ++i) f[i] = k_at(i);
+#pragma unroll
+            for (int i = 0; i < 2 * NQ; ++i)
+                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i], qf[i >> 1], s[i & 1], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedRead, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * NQ - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, kAhead, 0);
         }
+        f16x8 vf[4 * ND];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) vf[i] = v_at(i);
         if (vs > vref) {
             const float f = vref * __builtin_amdgcn_rcpf(vs);
             vref = vs;
@@ -125,8 +148,8 @@ struct TileState {
         // score (g, k) is token j0 + 32 g + 16 hf + k
         const int a0 = lo - j0 - 16 * hf, a1 = hi - j0 - 16 * hf;
         if (j0 + kKvBlock > min_hi || j0 < max_lo) {
-            mask_scores<16>(s[0], a0, a1, 0);
-            mask_scores<16>(s[1], a0, a1, 32);
+            mask_scores(s[0], a0, a1);
+            mask_scores(s[1], a0 - 32, a1 - 32);
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -148,32 +171,33 @@ struct TileState {
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int k = 0; k < 16; ++k) s[g][k] = __builtin_amdgcn_exp2f(fmaf(s[g][k], c, b));
-        if (!(ks < INFINITY && vs < INFINITY)) {
-            bad_weights<16>(s[0], a0, a1, 0);
-            bad_weights<16>(s[1], a0, a1, 32);
-        }
         float sum = 0.0f;
+        f16x8 pf[4];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int st = 0; st < 4; ++st) {
+            u32x4v pw;
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                u32x4v pw;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    sum += s[g][8 * st + 2 * k];
-                    sum += s[g][8 * st + 2 * k + 1];
-                    pw[k] = pack_f16(s[g][8 * st + 2 * k], s[g][8 * st + 2 * k + 1]);
-                }
-                const f16x8 pf = __builtin_bit_cast(f16x8, pw);
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const f16x8 vf =
-                        *reinterpret_cast<const f16x8*>(vl + (((g * 2 + st) * ND + d) * 64 + lane) * 16);
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, acc[d], 0, 0, 0);
-                }
+            for (int k = 0; k < 4; ++k) {
+                const float p0 = s[st >> 1][8 * (st & 1) + 2 * k], p1 = s[st >> 1][8 * (st & 1) + 2 * k + 1];
+                sum += p0;
+                sum += p1;
+                pw[k] = pack_f16(p0, p1);
             }
+            pf[st] = __builtin_bit_cast(f16x8, pw);
         }
+#pragma unroll
+        for (int i = kAhead; i < 4 * ND; ++i) vf[i] = v_at(i);
+#pragma unroll
+        for (int i = 0; i < 4 * ND; ++i)
+            acc[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i], pf[i / ND], acc[i % ND], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * ND - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, kAhead, 0);
         l = fmaf(sum, inv_r, l);
+        if (bad_scales(ks, vs)) l = bad_sum(l, lo, hi, j0);
     }
 
     __device__ __forceinline__ void finish() { l += __shfl_xor(l, 32, 64); }
@@ -264,6 +288,9 @@ __device__ __forceinline__ void walk(const KvAttnArgs& a, const KvRequest& q, in
         refs.blk = -1;
         refs.ks = refs.vs = 0.0f;
         if (i + lane < nb) refs = kv_block_ref(a, r, b0 + i + lane, h);
+        // Wait for them here, not wherever the paths meet again (which would wait
+        // for every code on its way as well).
+        asm volatile("" : "+v"(refs.blk), "+v"(refs.ks), "+v"(refs.vs));
     };
     auto next = [&](int i, KvBlockRef& b) {
         for (; i < nb; ++i) {
@@ -298,12 +325,17 @@ void k_attention_tiles(KvAttnArgs a, int64_t* __restrict__ plan, float* __restri
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kKvBlock * D * 2 * 2];
     TileState<KT, D> st;
     if constexpr (!SHARES) {
-        // One pair a workgroup, head fastest, the last rows (which see the most
-        // blocks) first.
-        const int64_t x = (int64_t)gridDim.x - 1 - blockIdx.x;
-        const int h = a.c.Hk - 1 - (int)(x % a.c.Hk);
+        // One pair a workgroup, head fastest.  The slots are taken as R columns of
+        // equal length, from the bottom row up: with requests of like lengths that
+        // is every request's last rows first, which see the most blocks, so that
+        // long pairs do not start last.
+        const int64_t S = kv_slots(a.c.T, a.c.R, a.G, kTilesTile), len = (S + a.c.R - 1) / a.c.R;
+        const int64_t x = blockIdx.x / a.c.Hk;
+        const int h = (int)(blockIdx.x % a.c.Hk);
+        const int64_t slot = (x % a.c.R) * len + (len - 1 - x / a.c.R);
+        if (slot >= S) return;
         int64_t tile;
-        const int64_t r = kv_slot_request<kTilesTile>(a, x / a.c.Hk, tile);
+        const int64_t r = kv_slot_request<kTilesTile>(a, slot, tile);
         const KvRequest q = kv_request(a, r);
         if (tile < 0 || tile * kTilesTile >= (int64_t)q.n * a.G) return;
         st.start(a, q, tile, h);
@@ -343,7 +375,7 @@ hipError_t tiles_of(const KvAttnArgs& a, bool shares, hipStream_t s) {
     if (shares) {
         k_attention_tiles<KT, D, true><<<kTilesShares, kThreads, 0, s>>>(a, plan, parts);
     } else {
-        const int64_t grid = kv_slots(a.c.T, a.c.R, a.G, kTilesTile) * a.c.Hk;
+        const int64_t grid = ceil_div(kv_slots(a.c.T, a.c.R, a.G, kTilesTile), a.c.R) * a.c.R * a.c.Hk;
         k_attention_tiles<KT, D, false><<<(unsigned)grid, kThreads, 0, s>>>(a, plan, parts);
     }
     return hipGetLastError();
