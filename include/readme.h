@@ -835,8 +835,8 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *   themselves, 2^-32 below 2^-21), so o is the exact result up to about
  *   2^-11 of the largest |v| the row sees plus its rounding to bf16.  The
  *   order of the sums depends on the sizes and lens, never on timing.
- *   A row of q with an infinity or a NaN gives an unspecified row; a NaN scale
- *   gives NaN in the rows that see any of its tokens.
+ *   A row of q with an infinity or a NaN gives an unspecified row; a scale
+ *   that is NaN or infinite gives NaN in the rows that see any of its tokens.
  *   q [T][ld_q] bf16 (head g at columns D g ..), o [T][ld_o] bf16 out, causal
  *   0 or 1, window >= 0, scale > 0 and finite; workspace >=
  *   readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks) bytes,
@@ -844,7 +844,8 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *   workspaces of their own.  o must not overlap q.
  *
  * All require D of 64, 128 or 256, 1 <= Hk <= 65535, H a multiple of Hk,
- * R <= 2^22, T H / Hk <= 2^27, row strides at least the row's width and 16-byte
+ * R <= 2^22, T H / Hk <= 2^27 (for the attention also T H / 16 + R Hk <= 2^23),
+ * row strides at least the row's width and 16-byte
  * multiples, arrays of rows 16-byte aligned; T = 0 enqueues nothing, else
  * R >= 1, max_blocks >= 1 and n_blocks >= 1.  The size queries return 0 for
  * arguments outside that set.

@@ -9,20 +9,20 @@ namespace readme {
 namespace {
 
 // Joins the parts of each pair that several workgroups shared, and zeroes the
-// rows of a request that sees no block.  One workgroup per (1024 / D rows of a
-// tile slot, head); a thread takes four dims of one row, four parts at a time in
+// rows of a request that sees no block.  One workgroup per (tile slot, head,
+// 1024 / D rows); a thread takes four dims of one row, four parts at a time in
 // flight.
 template <int D, int ROWS>
 __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int64_t* __restrict__ plan,
                                                         const float* __restrict__ parts) {
     constexpr int kPart = kv_part_floats<D, ROWS>;
-    constexpr int kStep = 1024 / D, kSteps = ROWS / kStep;
+    constexpr int kStep = 1024 / D;
     const int h = blockIdx.y;
     int64_t tl;
-    const int64_t r = kv_slot_request<ROWS>(a, blockIdx.x / kSteps, tl);
+    const int64_t r = kv_slot_request<ROWS>(a, blockIdx.x, tl);
     const KvRequest q = kv_request(a, r);
     const KvPlan p = kv_plan<ROWS>(a, q);
-    const int i = (int)(blockIdx.x % kSteps) * kStep + threadIdx.x / (D / 4);
+    const int i = (int)blockIdx.z * kStep + threadIdx.x / (D / 4);
     const int64_t row = tl * ROWS + i;
     if (tl < 0 || row >= (int64_t)q.n * a.G) return;
     const int d = threadIdx.x % (D / 4) * 4;
@@ -73,7 +73,7 @@ hipError_t join_of(const KvAttnArgs& a, hipStream_t s) {
     const int64_t* plan = reinterpret_cast<const int64_t*>(a.ws);
     const float* parts =
         reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.ws) + kv_plan_bytes(a.c.R));
-    const dim3 grid((unsigned)(kv_slots(a.c.T, a.c.R, a.G, ROWS) * (ROWS * D / 1024)), (unsigned)a.c.Hk);
+    const dim3 grid((unsigned)kv_slots(a.c.T, a.c.R, a.G, ROWS), (unsigned)a.c.Hk, ROWS * D / 1024);
     k_attention_join<D, ROWS><<<grid, 256, 0, s>>>(a, plan, parts);
     return hipGetLastError();
 }
@@ -102,29 +102,34 @@ hipError_t launch_join(const KvAttnArgs& a, int rows, hipStream_t s) {
 //   2000 rows on 8 blocks           rows/2 16, tiles/1 19; 240 on 47: rows/8 19, tiles/0 34
 //   8 x 800 rows on 4 blocks        tiles/1 17, rows/1 29, tiles/0 29
 //   8000 rows on 32 blocks          tiles/1 57, tiles/0 80, rows/1 132
+//   decode, 357 pairs of a table of 159 blocks, 4 seen through a window: rows/4 9,
+//                                   rows/0 14
 //   16 x 64 rows on 63 blocks, 192 tile pairs: tiles/0 56, tiles/1 98
 struct Form {
     int rows, waves;
 };
 
-Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t max_blocks) {
+// `blocks`: at most so many of a request's blocks are seen.
+Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks) {
     const int64_t rows = T * G;
     const int64_t pairs = kv_slots(T, R, G, kRowsTile) * Hk;
     const int64_t tile_pairs = kv_slots(T, R, G, kTilesTile) * Hk;
-    const bool brief = max_blocks <= 64;
+    const bool brief = blocks <= 64;
     // Few rows a request, or few tiles, or little to gain from sharing keys
     if (rows <= R * (D == 64 ? 32 : 16) || (brief && (tile_pairs < 256 || rows < R * 48))) {
         if (!brief) return {kRowsTile, 0};
         // As many waves as fit the chip together, and as there are blocks
         int w = 1;
-        while (w < 8 && pairs * w * 2 <= (D == 256 ? 1280 : 2560) && w < max_blocks) w *= 2;
+        while (w < 8 && pairs * w * 2 <= (D == 256 ? 1280 : 2560) && w < blocks) w *= 2;
         return {kRowsTile, w};
     }
-    return {kTilesTile, tile_pairs >= 384 || max_blocks <= 16 ? 1 : 0};
+    return {kTilesTile, tile_pairs >= 384 || blocks <= 16 ? 1 : 0};
 }
 
 }  // namespace
 
+// Enough for any window: one that bounds the blocks turns shares into whole pairs,
+// never the other way.
 size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks) {
     const Form f = form_of(T, R, H / Hk, Hk, D, max_blocks);
     const int64_t grid = f.waves ? 0 : f.rows == kTilesTile ? kTilesShares : kRowsShares;
@@ -132,7 +137,10 @@ size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_
 }
 
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {
-    const Form f = form_of(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, a.c.max_blocks);
+    // A request's rows, at most T, lie one after the other
+    int64_t blocks = a.c.max_blocks;
+    if (a.window > 0 && (a.window + a.c.T) / kKvBlock + 2 < blocks) blocks = (a.window + a.c.T) / kKvBlock + 2;
+    const Form f = form_of(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, blocks);
     const hipError_t e = f.rows == kTilesTile ? launch_attention_tiles(kt, a, f.waves == 0, s)
                                               : launch_attention_rows(kt, a, f.waves, s);
     return e != hipSuccess || f.waves ? e : launch_join(a, f.rows, s);

@@ -382,8 +382,11 @@ __device__ __forceinline__ KvBlockRef kv_block_ref(const KvAttnArgs& a, int64_t 
     if (b.blk >= 0) {
         const float2 sc =
             *reinterpret_cast<const float2*>(a.c.scales + ((int64_t)b.blk * a.c.Hk + h) * 2);
-        b.ks = sc.x;
-        b.vs = sc.y;
+        // An infinite scale counts as NaN: as the largest value scale so far it
+        // would empty the sums of rows that do not see its block.
+        const bool bad = bad_scales(sc.x, sc.y);
+        b.ks = bad ? __builtin_nanf("") : sc.x;
+        b.vs = bad ? __builtin_nanf("") : sc.y;
     }
     return b;
 }

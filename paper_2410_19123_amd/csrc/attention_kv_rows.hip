@@ -277,7 +277,7 @@ __device__ __forceinline__ void join_waves(const KvAttnArgs& a, const KvRequest&
         xl[wv * kRows + col] = st.l;
     }
     __syncthreads();
-        float f[W], mx = -INFINITY, l = 0.0f;
+    float f[W], mx = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) mx = fmaxf(mx, xm[w * kRows + col]);
     const float base = mx == -INFINITY ? 0.0f : mx;

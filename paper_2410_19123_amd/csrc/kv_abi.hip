@@ -10,7 +10,13 @@ using namespace readme;
 namespace {
 
 constexpr int64_t kMaxRequests = 1 << 22;
-constexpr int64_t kMaxRows = 1 << 27;  // T H / Hk: grids stay below 2^32 threads
+constexpr int64_t kMaxRows = 1 << 27;   // T H / Hk
+// Tiles of 16 query rows times key heads: the attention grids, a workgroup of
+// up to 256 threads for each, stay below 2^32 threads.
+constexpr int64_t kMaxPairs = 1 << 23;
+// Every position is below 2^31, and 2^27 rows may lie before the first: a window
+// beyond this is none, and positions less it fit 64 bits.
+constexpr int64_t kMaxWindow = 1ll << 33;
 
 inline readme_status st_of(hipError_t e) { return e == hipSuccess ? README_OK : README_ERR_HIP; }
 inline bool al(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -35,6 +41,13 @@ readme_status check_sizes(readme_kv_type kt, int64_t T, int32_t R, int32_t H, in
     if (H % Hk != 0) return README_ERR_ARG;
     if (T > kMaxRows / (H / Hk)) return README_ERR_UNSUPPORTED;
     return README_OK;
+}
+
+readme_status check_attention(int64_t T, int32_t R, int32_t H, int32_t Hk, int32_t D,
+                              readme_kv_type kt, int64_t max_blocks, int64_t n_blocks, bool* done) {
+    const readme_status st = check_sizes(kt, T, R, H, Hk, D, max_blocks, n_blocks, done);
+    if (st != README_OK || *done) return st;
+    return (T * (H / Hk) / 16 + R) * Hk > kMaxPairs ? README_ERR_UNSUPPORTED : README_OK;
 }
 
 readme_status check_cache(const KvCacheArgs& c) {
@@ -121,7 +134,7 @@ readme_status readme_kv_read(readme_kv_type kt, readme_dtype dt, int64_t T, int3
 size_t readme_attention_kv_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk, int32_t D,
                                            int64_t max_blocks) {
     bool done;
-    if (check_sizes(README_KV_I8, T, R, H, Hk, D, max_blocks, 1, &done) != README_OK || done)
+    if (check_attention(T, R, H, Hk, D, README_KV_I8, max_blocks, 1, &done) != README_OK || done)
         return 0;
     return kv_attention_workspace(T, R, H, Hk, D, max_blocks);
 }
@@ -137,7 +150,7 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
     if (causal < 0 || causal > 1 || window < 0 || !(score > 0.0f) || !isfinite(score))
         return README_ERR_ARG;
     bool done;
-    readme_status st = check_sizes(kt, T, R, H, Hk, D, max_blocks, n_blocks, &done);
+    readme_status st = check_attention(T, R, H, Hk, D, kt, max_blocks, n_blocks, &done);
     if (st != README_OK || done) return st;
     const KvCacheArgs c = cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
                                      scales);
@@ -157,7 +170,7 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
     a.G = H / Hk;
     a.score = score;
     a.causal = causal;
-    a.window = window;
+    a.window = window < kMaxWindow ? window : kMaxWindow;
     a.ws = workspace;
     return st_of(launch_kv_attention(kt, a, as_stream(stream)));
 }

@@ -96,6 +96,28 @@ def test_attention_refuses(lib, bad, status):
     assert _attention(lib, **bad) == status
 
 
+@pytest.mark.parametrize("T,R,H,Hk", [
+    (1 << 27, 1, 8, 8),              # row tiles times heads past the grids
+    (1 << 20, 1 << 20, 64, 64),      # and requests times heads
+    (16, 1 << 22, 8, 8),
+    (16, 129, 65535, 65535),
+])
+def test_attention_refuses_what_its_grids_cannot_hold(lib, T, R, H, Hk):
+    assert _attention(lib, T=T, R=R, H=H, Hk=Hk, ld_q=H * 128, ld_o=H * 128) == 2
+    assert lib.readme_attention_kv_workspace_bytes(T, R, H, Hk, 128, 4) == 0
+
+
+def test_a_window_needs_no_more_workspace(lib):
+    """The workspace query knows no window; a call with one takes what it
+    says for the same sizes (any smaller one is refused)."""
+    w = lib.readme_attention_kv_workspace_bytes
+    for T, R, mb in ((64, 64, 2000), (4096, 4, 2000), (1000, 3, 40), (1 << 23, 1, 1 << 20)):
+        need = w(T, R, 8, 8, 128, mb)
+        assert need > 0
+        for window in (0, 1, 1000, (1 << 63) - 1):
+            assert _attention(lib, T=T, R=R, H=8, Hk=8, mb=mb, window=window, wsb=need - 1) == 3
+
+
 def test_python_form_refuses():
     from paper_2410_19123_amd import _lib as L
     i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731

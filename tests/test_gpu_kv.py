@@ -405,6 +405,54 @@ def test_nan_scales_reach_only_their_readers():
         assert not torch.isnan(o.view(3, new, 64)[:, pos >= 137]).any()
 
 
+@pytest.mark.parametrize("new", [1, 90])
+def test_infinite_scales_count_as_nan(new):
+    """The rows that see the block become NaN, the others keep their values."""
+    L = _lib()
+    off, lens = _i32(_offsets([new] * 2)), _i32([300, 300])
+    q = torch.randn(2 * new, 256, device="cuda:0").bfloat16()
+    for half in (0, 1):
+        c = _random_cache("e4m3", 2, 1, 128, 5, seed=25)
+        for window in (0, 40):
+            was = L.readme_attention_kv(1, q, off, lens, *c.args(), H=2, window=window)
+            scales = c.scales.clone()
+            c.scales[int(c.table[0, 3]), 0, half] = float("inf")   # positions 192 .. 255
+            now = L.readme_attention_kv(1, q, off, lens, *c.args(), H=2, window=window)
+            c.scales.copy_(scales)
+            pos = torch.arange(300 - new, 300, device="cuda:0")
+            sees = (pos >= 192) & ((pos - window < 255) if window else True)
+            sees = torch.cat([sees, torch.zeros_like(sees)])
+            assert torch.isnan(now[sees].float()).all()
+            # Twice what _attend allows, of the largest value any block can hold
+            tol = 2 * (2.0 ** -8 * was.float().abs() + 2.0 ** -10 * 448 * float(scales[..., 1].max()))
+            assert ((now.float() - was.float()).abs() <= tol)[~sees].all()
+            assert not torch.isnan(was.float()).any()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [1 << 40, (1 << 63) - 1])
+def test_a_window_past_everything(causal, window):
+    """More rows than tokens: rows before position 0 lie within any long window
+    of the tokens after them."""
+    new, lens = [40, 3], [5, 400]
+    c = _random_cache("i8", 2, 1, 64, 7, seed=26)
+    _attend(c, new, lens, 2, causal, window)
+    assert torch.equal(_attend(c, new, lens, 2, causal, window, q=torch.ones(43, 2, 64).bfloat16())[1],
+                       _attend(c, new, lens, 2, causal, 0, q=torch.ones(43, 2, 64).bfloat16())[1])
+
+
+@pytest.mark.parametrize("kt,D", [("i8", 64), ("e4m3", 128), ("i8", 256)])
+@pytest.mark.parametrize("new", [[1] * 5, [1, 0, 40, 7, 2], [300, 200]])
+def test_windows_of_long_tables(kt, D, new):
+    """A table of many blocks of which the window shows few."""
+    R = len(new)
+    c = _random_cache(kt, R, 1, D, 90, seed=27)
+    lens = [90 * 64, 3, 4000, 64, 5001][:R]
+    lens = [max(a, b) for a, b in zip(lens, new)]
+    for window in (1, 64, 65, 900):
+        _attend(c, new, lens, 3, True, window)
+
+
 @pytest.mark.parametrize("R,lens", [(1, [40000]), (3, [20000, 1, 9000]), (70, None)])
 def test_attention_long_and_uneven(R, lens):
     """Work split over the keys and joined: against float64 torch on the GPU."""
