@@ -28,6 +28,7 @@ namespace readme {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // 16 consecutive values of a row, as they are stored.
 template <int DT>
@@ -49,6 +50,25 @@ struct Row16 {
         const uint32_t w = (d & 3) == 0 ? q.x : (d & 3) == 1 ? q.y : (d & 3) == 2 ? q.z : q.w;
         if constexpr (DT == README_F32) return __uint_as_float(w);
         return k & 1 ? bf16_hi(w) : bf16_lo(w);
+    }
+    // Bits of the largest magnitude, a NaN above every number.
+    __device__ __forceinline__ uint32_t most() const {
+        if constexpr (DT == README_F32) {
+            uint32_t m = 0;
+#pragma unroll
+            for (auto& q : v)
+                m = max(m, max(max(q.x & 0x7fffffffu, q.y & 0x7fffffffu),
+                               max(q.z & 0x7fffffffu, q.w & 0x7fffffffu)));
+            return m;
+        } else {
+            u16x2 m = {0, 0};
+#pragma unroll
+            for (auto& q : v)
+#pragma unroll
+                for (const uint32_t w : {q.x, q.y, q.z, q.w})
+                    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w & 0x7fff7fffu));
+            return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+        }
     }
 };
 
@@ -78,32 +98,72 @@ __device__ __forceinline__ uint32_t e4m3_byte(float x) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, 0.0f, 0, false) & 0xffu;
 }
 
-// The code byte nearest to x / s (inv = 1 / s in fp32), ties to even.
-//   int8: n = rint(x * inv) is at most one off; x - n s is exact in fp32 (a
-//   multiple of s's last place and at most 1.5 s, or x near s), so comparing
-//   it with s / 2 settles n.
-//   e4m3: one Newton step makes q faithful (less than one unit off), the sign
-//   of x - q s tells on which side x / s lies, and taking the neighbour with
-//   an odd last bit (round to odd) keeps the hardware's second rounding from
-//   seeing a tie where there is none.
-template <int KT>
-__device__ __forceinline__ uint32_t encode(float x, float s, float inv) {
-    if constexpr (KT == README_KV_I8) {
-        float n = rintf(x * inv);
-        const float r = fmaf(-n, s, x), h = 0.5f * s;
-        const bool odd = ((int)n & 1) != 0;
-        if (r > h || (r == h && odd)) n += 1.0f;
-        else if (r < -h || (r == -h && odd)) n -= 1.0f;
-        n = fminf(fmaxf(n, -127.0f), 127.0f);
-        return (uint32_t)((int)n + 128);
-    } else {
-        float q = x * inv;
-        q = fmaf(fmaf(-q, s, x), inv, q);
-        const float r = fmaf(-q, s, x);
-        uint32_t u = __float_as_uint(q);
-        if (r != 0.0f && !(u & 1u)) u = ((r > 0.0f) == (q > 0.0f)) ? u + 1u : u - 1u;
-        if (q == 0.0f) u = 0u;
-        return e4m3_byte(fminf(fmaxf(__uint_as_float(u), -448.0f), 448.0f));
+// x / s (inv = 1 / s in fp32) rounded to odd: one Newton step makes q faithful
+// (less than one unit off), the sign of x - q s tells on which side x / s lies,
+// and taking the neighbour with an odd last bit keeps a second rounding, to e4m3,
+// from seeing a tie where there is none.
+__device__ __forceinline__ float quotient_odd(float x, float s, float inv) {
+    float q = x * inv;
+    q = fmaf(fmaf(-q, s, x), inv, q);
+    const float r = fmaf(-q, s, x);
+    uint32_t u = __float_as_uint(q);
+    if (r != 0.0f && !(u & 1u)) u = ((r > 0.0f) == (q > 0.0f)) ? u + 1u : u - 1u;
+    if (q == 0.0f) u = 0u;
+    return __uint_as_float(u);
+}
+
+// The int8 code nearest to x / s, plus 128, ties to even: n = rint(x inv) is at
+// most one off; x - n s is exact in fp32 (a multiple of s's last place and at
+// most 1.5 s, or x near s), so comparing it with s / 2 settles n.
+__device__ __forceinline__ uint32_t nearest_i8(float x, float s, float inv) {
+    float n = rintf(x * inv);
+    const float r = fmaf(-n, s, x), h = 0.5f * s;
+    const bool odd = ((int)n & 1) != 0;
+    if (r > h || (r == h && odd)) n += 1.0f;
+    else if (r < -h || (r == -h && odd)) n -= 1.0f;
+    n = fminf(fmaxf(n, -127.0f), 127.0f);
+    return (uint32_t)((int)n + 128);
+}
+
+// Codes of a row's 16 values.  The plain product q = x inv is within 2 units in
+// its last place of x / s, so its nearest code is the quotient's unless a tie
+// between two codes lies that near.  Such values are settled one by one: bf16
+// rows hold many ties of one kind (half of the largest element is 63.5 int8
+// codes), so a whole row would rarely go without.  The write of 16155 rows of 8
+// heads of 128 takes 27 us this way, 36 with rows settled whole, 33 with every
+// value settled.
+//   int8: adding 1.5 2^23 rounds q to an integer, ties to even, and leaves code
+//   + 128 in the low byte; |q| <= 127, so 2 units are at most 2^-16.
+//   e4m3: from 2^-6 on a tie is the middle of the 20 mantissa bits that a code
+//   does not have; smaller quotients all go the long way.
+template <int KT, int DT>
+__device__ __forceinline__ void encode16(const Row16<DT>& x, float s, float inv, uint32_t (&w)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (KT == README_KV_I8) {
+            constexpr float kRound = 12582912.0f + 128.0f;
+            uint32_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = x.at(4 * k + e), q = v * inv, f = q + kRound;
+                u[e] = __float_as_uint(f);
+                if (fabsf(q - (f - kRound)) > 0.5f - 0x1p-15f) u[e] = nearest_i8(v, s, inv);
+            }
+            w[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u),
+                                         __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
+        } else {
+            float c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = x.at(4 * k + e), q = v * inv;
+                c[e] = q;
+                if (((__float_as_uint(q) + 0x80003u) & 0xfffffu) <= 6u || fabsf(q) < 0x1p-6f)
+                    c[e] = quotient_odd(v, s, inv);
+                c[e] = fminf(fmaxf(c[e], -448.0f), 448.0f);
+            }
+            const int b = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+            w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], b, true);
+        }
     }
 }
 
@@ -254,9 +314,7 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
         if (p * RPP + rw < b.n) x[p].load(src, (b.tok + p * RPP + rw) * ld + col);
     }
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) am = max(am, __float_as_uint(x[p].at(k)) & 0x7fffffffu);
+    for (int p = 0; p < NP; ++p) am = max(am, x[p].most());
     am = wave_max_u32(am);
     __syncthreads();  // an earlier block's reads of `most` and `lds` are over
     if (lane == 0) most[tid >> 6] = am;
@@ -306,13 +364,10 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
         const int i = p * RPP + rw;
         if (i >= b.n) break;
         uint32_t w[4];
+        encode16<KT, DT>(x[p], s, inv, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            w[k] = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[k] |= encode<KT>(x[p].at(4 * k + e), s, inv) << (8 * e);
+        for (int k = 0; k < 4; ++k)
             if (bad) w[k] = KT == README_KV_I8 ? 0x80808080u : 0u;
-        }
         if constexpr (!V) {
             *reinterpret_cast<uint4*>(dst + kv_k_byte(D, b.slot + i, ch * 16)) =
                 make_uint4(w[0], w[1], w[2], w[3]);
