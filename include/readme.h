@@ -811,13 +811,13 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *             call's, else scale * 2^k with the least k >= 0 for which it is
  *             at least need; the earlier codes c become round(c 2^-k);
  *     code  = round(x / scale), the exact quotient;
- *   both to the nearest code, ties to even.  However often a block grows an
- *   earlier value is off by less than one step of I8's final scale.  If x
- *   holds an infinity or a NaN, or the earlier tokens' scale is not positive
- *   and finite, the scale becomes NaN: every value read from that (block,
- *   head, K or V) is NaN until its first token is written again.  Rows at
- *   absent positions are dropped.  Writing the same rows again changes
- *   nothing.
+ *   both to the nearest code, ties to even (E4M3's zero may have either sign).
+ *   However often a block grows an earlier value is off by less than one step
+ *   of I8's final scale.  If x holds an infinity or a NaN, or the earlier
+ *   tokens' scale is not positive and finite, the scale becomes NaN: every
+ *   value read from that (block, head, K or V) is NaN until its first token is
+ *   written again.  Rows at absent positions are dropped.  Writing the same
+ *   rows again changes nothing.
  *
  * readme_kv_read -- the rows back: k, v [T][ld] dt (outputs), value = code *
  *   scale in fp32, rounded once to dt; zeros at absent positions.  Reading
@@ -871,6 +871,32 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
                                   float scale, int32_t causal, int64_t window, void *o,
                                   int64_t ld_o, void *workspace, size_t workspace_bytes,
                                   void *stream);
+
+/*
+ * readme_router_tf_cached -- readme_router_tf over the call's tokens only, those
+ * before them in the cache: request r's tokens are the last of its lens[r],
+ * their positions lens[r] - n_r + i; their rotated keys and their values go
+ * into the cache (readme_kv_write: D / 128 heads of 128, none shared) and the
+ * attention reads all of it (readme_attention_kv, causal, scale 1 / sqrt(128)).
+ * A prompt is a call in which every token is new, a decode step one of a token
+ * per request; a prompt may come in pieces.  req_offsets, as in
+ * readme_router_tf from 0 to T, are the cache's offsets; everything else is as
+ * in the two, the workspace's regions among it (README_RTF_POS holds the
+ * positions in the request, README_RTF_OFFS {0, T}), with
+ * workspace >= readme_router_tf_cached_workspace_bytes(T, R, D, F, max_blocks)
+ * bytes.  A token at an absent position leaves no key, and one before position 0
+ * sees nothing.  Results differ from readme_router_tf's by the codes' rounding.
+ */
+size_t readme_router_tf_cached_workspace_bytes(int64_t T, int32_t R, int64_t D, int64_t F,
+                                               int64_t max_blocks);
+readme_status readme_router_tf_cached(readme_kv_type kt, int64_t T, int32_t R, int64_t D, int64_t F,
+                                      int32_t E, int64_t V, const int32_t *tokens,
+                                      const int32_t *req_offsets, const int32_t *lens,
+                                      const int32_t *table, int64_t max_blocks, int64_t n_blocks,
+                                      void *codes, float *scales, const void *emb,
+                                      const void *packed, const void *w_router, const float *bias,
+                                      float rms_eps, int32_t *expert_ids, float *logits,
+                                      void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

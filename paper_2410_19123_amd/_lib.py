@@ -99,6 +99,10 @@ SIGNATURES = {
                                _I64, _I64, _P, _P, _P]),
     "readme_kv_read": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _P, _P, _I64, _I64, _P, _P,
                               _P, _I64, _P, _I64, _P]),
+    "readme_router_tf_cached_workspace_bytes": (_SZ, [_I64, _I32, _I64, _I64, _I64]),
+    "readme_router_tf_cached": (_I32, [_I32, _I64, _I32, _I64, _I64, _I32, _I64, _P, _P, _P, _P,
+                                      _I64, _I64, _P, _P, _P, _P, _P, _P, _F, _P, _P, _P, _SZ,
+                                      _P]),
     "readme_attention_kv_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I64]),
     "readme_attention_kv": (_I32, [_I32, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P, _I64,
                                    _I64, _P, _P, _F, _I32, _I64, _P, _I64, _P, _SZ, _P]),
@@ -804,9 +808,9 @@ def _kv_cache_args(offsets, lens, table, codes, scales):
     if dev < 0:
         raise ValueError("libreadme takes device tensors")
     i32 = torch.int32
-    if offsets.dtype != i32 or lens.dtype != i32 or table.dtype != i32:
+    if offsets.dtype is not i32 or lens.dtype is not i32 or table.dtype is not i32:
         raise ValueError("offsets, lens and table must be int32")
-    if codes.dtype != torch.uint8 or scales.dtype != torch.float32:
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.float32:
         raise ValueError("codes must be uint8 and scales fp32")
     for t in (offsets, lens, table, codes, scales):
         if t.get_device() != dev:
@@ -842,7 +846,7 @@ def readme_kv_write(kt: int, k, v, offsets, lens, table, codes, scales) -> None:
     R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
     T = k.shape[0]
     ld_k, ld_v = _kv_rows(k, T, Hk * D, dev, "k"), _kv_rows(v, T, Hk * D, dev, "v")
-    if v.dtype != k.dtype:
+    if v.dtype is not k.dtype:
         raise ValueError("k and v dtypes disagree")
     _kv_call(dev, "readme_kv_write", kt, _dt(k), T, R, Hk, D, k.data_ptr(), ld_k, v.data_ptr(),
              ld_v, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb,
@@ -864,7 +868,7 @@ def readme_kv_read(kt: int, offsets, lens, table, codes, scales, k=None, v=None,
         v = v if v is not None else torch.empty((T, Hk * D), dtype=dtype, device=codes.device)
     T = k.shape[0]
     ld_k, ld_v = _kv_rows(k, T, Hk * D, dev, "k"), _kv_rows(v, T, Hk * D, dev, "v")
-    if v.dtype != k.dtype:
+    if v.dtype is not k.dtype:
         raise ValueError("k and v dtypes disagree")
     _kv_call(dev, "readme_kv_read", kt, _dt(k), T, R, Hk, D, offsets.data_ptr(), lens.data_ptr(),
              table.data_ptr(), mb, nb, codes.data_ptr(), scales.data_ptr(), k.data_ptr(), ld_k,
@@ -885,7 +889,7 @@ def readme_attention_kv(kt: int, q, offsets, lens, table, codes, scales, H: int,
     T = q.shape[0]
     if o is None:
         o = torch.empty((T, H * D), dtype=torch.bfloat16, device=codes.device)
-    if q.dtype != torch.bfloat16 or o.dtype != torch.bfloat16:
+    if q.dtype is not torch.bfloat16 or o.dtype is not torch.bfloat16:
         raise ValueError("q and o must be bf16")
     ld_q, ld_o = _kv_rows(q, T, H * D, dev, "q"), _kv_rows(o, T, H * D, dev, "o")
     if workspace is None:
@@ -898,6 +902,43 @@ def readme_attention_kv(kt: int, q, offsets, lens, table, codes, scales, H: int,
              scales.data_ptr(), D ** -0.5 if scale is None else scale, 1 if causal else 0, window,
              o.data_ptr(), ld_o, workspace.data_ptr(), workspace.nbytes)
     return o
+
+
+def readme_router_tf_cached_workspace_bytes(T: int, R: int, D: int, F: int,
+                                            max_blocks: int) -> int:
+    return int(load().readme_router_tf_cached_workspace_bytes(T, R, D, F, max_blocks))
+
+
+def readme_router_tf_cached(kt: int, tokens, req_offsets, lens, table, codes, scales, emb, packed, F,
+                            w_router, bias=None, rms_eps=1e-5, expert_ids=None, logits=None,
+                            workspace=None):
+    """The router G over the new tokens of requests whose earlier ones are in the
+    cache (readme_kv_cache with D / 128 heads of 128), which takes the new ones;
+    returns (expert_ids, logits or None, workspace) as readme_router_tf."""
+    R, Hk, hd, mb, nb, dev = _kv_cache_args(req_offsets, lens, table, codes, scales)
+    T = tokens.shape[0]
+    V, D = emb.shape
+    E = w_router.shape[0]
+    if tokens.dtype != torch.int32:
+        raise ValueError("tokens must be int32")
+    if emb.dtype != torch.bfloat16 or w_router.dtype != torch.bfloat16 or \
+            w_router.shape[1] != D:
+        raise ValueError("emb [V][D] and w_router [E][D] must be bf16")
+    if hd != 128 or Hk * 128 != D:
+        raise ValueError("the cache must have D / 128 heads of 128")
+    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != E):
+        raise ValueError("bias must be fp32 [E]")
+    if expert_ids is None:
+        expert_ids = torch.empty(T, dtype=torch.int32, device=codes.device)
+    if workspace is None:
+        ws = readme_router_tf_cached_workspace_bytes(T, R, D, F, mb)
+        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=codes.device)
+    _dev(tokens, codes, emb, packed, w_router, bias, expert_ids, logits, workspace)
+    _kv_call(dev, "readme_router_tf_cached", kt, T, R, D, F, E, V, _p(tokens), _p(req_offsets),
+             _p(lens), _p(table), mb, nb, _p(codes), _p(scales), _p(emb), _p(packed), _p(w_router),
+             _p(bias), rms_eps, _p(expert_ids), _p(logits), _p(workspace),
+             workspace.numel() * workspace.element_size())
+    return expert_ids, logits, workspace
 
 
 def readme_status_string(status: int) -> str:

@@ -43,14 +43,23 @@ readme_status check_sizes(readme_kv_type kt, int64_t T, int32_t R, int32_t H, in
     return README_OK;
 }
 
-readme_status check_attention(int64_t T, int32_t R, int32_t H, int32_t Hk, int32_t D,
-                              readme_kv_type kt, int64_t max_blocks, int64_t n_blocks, bool* done) {
+readme_status check_rows(const void* p, int64_t ld, int64_t width, int64_t elem) {
+    if (!p || !al(p, 16) || ld < width || (ld * elem) % 16 != 0) return README_ERR_ARG;
+    return README_OK;
+}
+
+}  // namespace
+
+namespace readme {
+
+readme_status kv_check_attention(readme_kv_type kt, int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                 int32_t D, int64_t max_blocks, int64_t n_blocks, bool* done) {
     const readme_status st = check_sizes(kt, T, R, H, Hk, D, max_blocks, n_blocks, done);
     if (st != README_OK || *done) return st;
     return (T * (H / Hk) / 16 + R) * Hk > kMaxPairs ? README_ERR_UNSUPPORTED : README_OK;
 }
 
-readme_status check_cache(const KvCacheArgs& c) {
+readme_status kv_check_cache(const KvCacheArgs& c) {
     if (!c.offsets || !c.lens || !c.table || !c.codes || !c.scales) return README_ERR_ARG;
     if (!al(c.offsets, 4) || !al(c.lens, 4) || !al(c.table, 4) || !al(c.codes, 16) ||
         !al(c.scales, 8))
@@ -58,12 +67,7 @@ readme_status check_cache(const KvCacheArgs& c) {
     return README_OK;
 }
 
-readme_status check_rows(const void* p, int64_t ld, int64_t width, int64_t elem) {
-    if (!p || !al(p, 16) || ld < width || (ld * elem) % 16 != 0) return README_ERR_ARG;
-    return README_OK;
-}
-
-KvCacheArgs cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int32_t* offsets,
+KvCacheArgs kv_cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int32_t* offsets,
                        const int32_t* lens, const int32_t* table, int64_t max_blocks,
                        int64_t n_blocks, const void* codes, const float* scales) {
     KvCacheArgs c{};
@@ -81,7 +85,7 @@ KvCacheArgs cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int32_
     return c;
 }
 
-}  // namespace
+}  // namespace readme
 
 extern "C" {
 
@@ -104,9 +108,9 @@ readme_status readme_kv_write(readme_kv_type kt, readme_dtype dt, int64_t T, int
     bool done;
     readme_status st = check_sizes(kt, T, R, Hk, Hk, D, max_blocks, n_blocks, &done);
     if (st != README_OK || done) return st;
-    const KvCacheArgs c = cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
+    const KvCacheArgs c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
                                      scales);
-    if ((st = check_cache(c)) != README_OK) return st;
+    if ((st = kv_check_cache(c)) != README_OK) return st;
     const int64_t es = (int64_t)dtype_size(dt), width = (int64_t)Hk * D;
     if ((st = check_rows(k, ld_k, width, es)) != README_OK) return st;
     if ((st = check_rows(v, ld_v, width, es)) != README_OK) return st;
@@ -122,9 +126,9 @@ readme_status readme_kv_read(readme_kv_type kt, readme_dtype dt, int64_t T, int3
     bool done;
     readme_status st = check_sizes(kt, T, R, Hk, Hk, D, max_blocks, n_blocks, &done);
     if (st != README_OK || done) return st;
-    const KvCacheArgs c = cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
+    const KvCacheArgs c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
                                      scales);
-    if ((st = check_cache(c)) != README_OK) return st;
+    if ((st = kv_check_cache(c)) != README_OK) return st;
     const int64_t es = (int64_t)dtype_size(dt), width = (int64_t)Hk * D;
     if ((st = check_rows(k, ld_k, width, es)) != README_OK) return st;
     if ((st = check_rows(v, ld_v, width, es)) != README_OK) return st;
@@ -134,7 +138,7 @@ readme_status readme_kv_read(readme_kv_type kt, readme_dtype dt, int64_t T, int3
 size_t readme_attention_kv_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk, int32_t D,
                                            int64_t max_blocks) {
     bool done;
-    if (check_attention(T, R, H, Hk, D, README_KV_I8, max_blocks, 1, &done) != README_OK || done)
+    if (kv_check_attention(README_KV_I8, T, R, H, Hk, D, max_blocks, 1, &done) != README_OK || done)
         return 0;
     return kv_attention_workspace(T, R, H, Hk, D, max_blocks);
 }
@@ -150,11 +154,11 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
     if (causal < 0 || causal > 1 || window < 0 || !(score > 0.0f) || !isfinite(score))
         return README_ERR_ARG;
     bool done;
-    readme_status st = check_attention(T, R, H, Hk, D, kt, max_blocks, n_blocks, &done);
+    readme_status st = kv_check_attention(kt, T, R, H, Hk, D, max_blocks, n_blocks, &done);
     if (st != README_OK || done) return st;
-    const KvCacheArgs c = cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
+    const KvCacheArgs c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
                                      scales);
-    if ((st = check_cache(c)) != README_OK) return st;
+    if ((st = kv_check_cache(c)) != README_OK) return st;
     const int64_t width = (int64_t)H * D;
     if ((st = check_rows(q, ld_q, width, 2)) != README_OK) return st;
     if ((st = check_rows(o, ld_o, width, 2)) != README_OK) return st;

@@ -88,6 +88,15 @@ struct KvCacheArgs {
     int Hk, D;
 };
 
+// The host checks of the entry points (kv_abi.hip), sizes before pointers.
+// `done`: there are no rows.
+readme_status kv_check_attention(readme_kv_type kt, int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                 int32_t D, int64_t max_blocks, int64_t n_blocks, bool* done);
+readme_status kv_check_cache(const KvCacheArgs& c);
+KvCacheArgs kv_cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int32_t* offsets,
+                          const int32_t* lens, const int32_t* table, int64_t max_blocks,
+                          int64_t n_blocks, const void* codes, const float* scales);
+
 hipError_t launch_kv_write(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c, const void* k,
                            int64_t ld_k, const void* v, int64_t ld_v, hipStream_t s);
 hipError_t launch_kv_read(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c, void* k,

@@ -24,6 +24,7 @@
 #include <limits.h>
 #include <math.h>
 
+#include "kv_cache.hpp"
 #include "router_common.hpp"
 
 namespace readme {
@@ -277,6 +278,17 @@ __global__ __launch_bounds__(256) void k_positions(int64_t T, int32_t R,
     for (int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < T;
          t += (int64_t)gridDim.x * blockDim.x)
         pos[t] = position_of(t, R, ro);
+}
+
+// The same where a request's tokens are the last of lens[r]: one workgroup per
+// request.
+__global__ __launch_bounds__(256) void k_cache_positions(int64_t T, const int32_t* __restrict__ ro,
+                                                         const int32_t* __restrict__ lens,
+                                                         int32_t* __restrict__ pos) {
+    int64_t lo, hi;
+    kv_rows(ro, T, blockIdx.x, lo, hi);
+    const int64_t first = (int64_t)lens[blockIdx.x] - (hi - lo);
+    for (int64_t t = lo + threadIdx.x; t < hi; t += blockDim.x) pos[t] = (int32_t)(first + t - lo);
 }
 
 // RoPE in place on NH heads of 128 bf16 values per row (row t at x + t*ld).
@@ -740,6 +752,91 @@ int64_t region_offset(int64_t T, int64_t D, int64_t F, int region) {
     return off;
 }
 
+// The block over the call's tokens; `cache`: over those in it as well, with
+// keys and values of kind kt and room for the attention behind the regions.
+hipError_t run_block(int64_t T, int32_t R, int64_t D, int64_t F, int32_t E, int64_t V,
+                     const int32_t* tokens, const int32_t* req_offsets, const KvCacheArgs* cache,
+                     readme_kv_type kt, const void* emb, const void* packed, const void* w_router,
+                     const float* bias, float rms_eps, int32_t* expert_ids, float* logits,
+                     void* workspace, hipStream_t s) {
+    char* ws = reinterpret_cast<char*>(workspace);
+    auto at = [&](int r) { return ws + region_offset(T, D, F, r); };
+    float* x = reinterpret_cast<float*>(at(README_RTF_X));
+    uint16_t* a = reinterpret_cast<uint16_t*>(at(README_RTF_A));
+    uint16_t* qkv = reinterpret_cast<uint16_t*>(at(README_RTF_QKV));
+    uint16_t* o = reinterpret_cast<uint16_t*>(at(README_RTF_O));
+    uint16_t* m = reinterpret_cast<uint16_t*>(at(README_RTF_M));
+    uint16_t* h = reinterpret_cast<uint16_t*>(at(README_RTF_H));
+    uint16_t* feat = reinterpret_cast<uint16_t*>(at(README_RTF_FEAT));
+    int32_t* pos = reinterpret_cast<int32_t*>(at(README_RTF_POS));
+    int32_t* offs = reinterpret_cast<int32_t*>(at(README_RTF_OFFS));
+    const char* pk = reinterpret_cast<const char*>(packed);
+    const int H = (int)(D / kHeadDim);
+
+    const bool wide = T * D >= (int64_t)4 << 20 && D <= 1024;
+    const void* mlp = pk + 4 * D * D * 2;
+    if (!cache && D == kFusedRouterWidth && padded_I(F) <= kFusedRouterMlp &&
+        T >= fused_router_tokens(F) && get_gemm_tile() == 0) {
+        hipError_t e = launch_router_head(T, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
+                                          offs, pk, qkv, s);
+        if (e == hipSuccess)
+            e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
+        if (e == hipSuccess)
+            e = launch_router_tail(T, F, E, rms_eps, o, pk + 3 * D * D * 2, mlp, w_router, bias, x,
+                                   m, h, feat, expert_ids, logits, s);
+        return e;
+    }
+    hipError_t e = launch_embed_norm(T, D, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
+                                     offs, s);
+    if (e == hipSuccess) {
+        GemmArgs g = plain_args(a, D, pk, 3 * D, offs, T, qkv, 3 * D);
+        g.tile = wide ? kTileQkv : 0;
+        e = launch_grouped_gemm(false, EPI_STORE, g, s);
+    }
+    if (e == hipSuccess && cache) {
+        k_cache_positions<<<(unsigned)R, 256, 0, s>>>(T, req_offsets, cache->lens, pos);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) e = launch_rope(T, 2 * H, pos, qkv, 3 * D, s);
+    if (e == hipSuccess && cache) {
+        e = launch_kv_write(kt, README_BF16, *cache, qkv + D, 3 * D, qkv + 2 * D, 3 * D, s);
+        KvAttnArgs kva{};
+        kva.c = *cache;
+        kva.q = qkv;
+        kva.ld_q = 3 * D;
+        kva.o = o;
+        kva.ld_o = D;
+        kva.G = 1;
+        kva.score = 1.4426950408889634f / sqrtf((float)kHeadDim);
+        kva.causal = 1;
+        kva.ws = at(README_RTF_END);
+        if (e == hipSuccess) e = launch_kv_attention(kt, kva, s);
+    } else if (e == hipSuccess) {
+        e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
+    }
+    if (e == hipSuccess) {
+        GemmArgs g = plain_args(o, D, pk + 3 * D * D * 2, D, offs, T, x, D);
+        g.tile = wide ? kTileNarrow : 0;
+        e = launch_grouped_gemm(false, EPI_RESID_ADD, g, s);
+    }
+    if (e == hipSuccess) e = launch_rms_rows(T, D, rms_eps, x, m, s);
+    if (e == hipSuccess) {
+        GemmArgs gu = gate_up_args(README_BF16, T, D, 1, F, m, offs, mlp, h);
+        gu.m_tiles32 = (int)ceil_div(T, 32);
+        gu.tile = wide ? kTileGateUp : 0;
+        e = launch_grouped_gemm(false, EPI_GATE_UP_SILU, gu, s);
+    }
+    if (e == hipSuccess) {
+        GemmArgs dn = down_args(README_BF16, T, D, 1, F, h, offs, mlp, x);
+        dn.m_tiles32 = (int)ceil_div(T, 32);
+        dn.tile = wide ? kTileNarrow : 0;
+        e = launch_grouped_gemm(false, EPI_RESID_ADD, dn, s);
+    }
+    if (e == hipSuccess)
+        e = launch_norm_gate(T, D, E, rms_eps, x, w_router, bias, feat, expert_ids, logits, s);
+    return e;
+}
+
 }  // namespace
 
 }  // namespace readme
@@ -831,65 +928,46 @@ readme_status readme_router_tf(int64_t T, int32_t R, int64_t D, int64_t F, int32
     if (!al16(emb) || !al16(packed) || !al16(w_router) || !al16(workspace)) return README_ERR_ARG;
     if (workspace_bytes < readme_router_tf_workspace_bytes(T, D, F)) return README_ERR_WORKSPACE;
 
-    hipStream_t s = as_stream(stream);
-    char* ws = reinterpret_cast<char*>(workspace);
-    auto at = [&](int r) { return ws + region_offset(T, D, F, r); };
-    float* x = reinterpret_cast<float*>(at(README_RTF_X));
-    uint16_t* a = reinterpret_cast<uint16_t*>(at(README_RTF_A));
-    uint16_t* qkv = reinterpret_cast<uint16_t*>(at(README_RTF_QKV));
-    uint16_t* o = reinterpret_cast<uint16_t*>(at(README_RTF_O));
-    uint16_t* m = reinterpret_cast<uint16_t*>(at(README_RTF_M));
-    uint16_t* h = reinterpret_cast<uint16_t*>(at(README_RTF_H));
-    uint16_t* feat = reinterpret_cast<uint16_t*>(at(README_RTF_FEAT));
-    int32_t* pos = reinterpret_cast<int32_t*>(at(README_RTF_POS));
-    int32_t* offs = reinterpret_cast<int32_t*>(at(README_RTF_OFFS));
-    const char* pk = reinterpret_cast<const char*>(packed);
-    const int H = (int)(D / kHeadDim);
+    return st_of(run_block(T, R, D, F, E, V, tokens, req_offsets, nullptr, 0, emb, packed, w_router,
+                           bias, rms_eps, expert_ids, logits, workspace, as_stream(stream)));
+}
 
-    const bool wide = T * D >= (int64_t)4 << 20 && D <= 1024;
-    const void* mlp = pk + 4 * D * D * 2;
-    if (D == kFusedRouterWidth && padded_I(F) <= kFusedRouterMlp && T >= fused_router_tokens(F) &&
-        get_gemm_tile() == 0) {
-        hipError_t e = launch_router_head(T, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
-                                          offs, pk, qkv, s);
-        if (e == hipSuccess)
-            e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
-        if (e == hipSuccess)
-            e = launch_router_tail(T, F, E, rms_eps, o, pk + 3 * D * D * 2, mlp, w_router, bias, x,
-                                   m, h, feat, expert_ids, logits, s);
-        return st_of(e);
-    }
-    hipError_t e = launch_embed_norm(T, D, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
-                                     offs, s);
-    if (e == hipSuccess) {
-        GemmArgs g = plain_args(a, D, pk, 3 * D, offs, T, qkv, 3 * D);
-        g.tile = wide ? kTileQkv : 0;
-        e = launch_grouped_gemm(false, EPI_STORE, g, s);
-    }
-    if (e == hipSuccess) e = launch_rope(T, 2 * H, pos, qkv, 3 * D, s);
-    if (e == hipSuccess)
-        e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
-    if (e == hipSuccess) {
-        GemmArgs g = plain_args(o, D, pk + 3 * D * D * 2, D, offs, T, x, D);
-        g.tile = wide ? kTileNarrow : 0;
-        e = launch_grouped_gemm(false, EPI_RESID_ADD, g, s);
-    }
-    if (e == hipSuccess) e = launch_rms_rows(T, D, rms_eps, x, m, s);
-    if (e == hipSuccess) {
-        GemmArgs gu = gate_up_args(README_BF16, T, D, 1, F, m, offs, mlp, h);
-        gu.m_tiles32 = (int)ceil_div(T, 32);
-        gu.tile = wide ? kTileGateUp : 0;
-        e = launch_grouped_gemm(false, EPI_GATE_UP_SILU, gu, s);
-    }
-    if (e == hipSuccess) {
-        GemmArgs dn = down_args(README_BF16, T, D, 1, F, h, offs, mlp, x);
-        dn.m_tiles32 = (int)ceil_div(T, 32);
-        dn.tile = wide ? kTileNarrow : 0;
-        e = launch_grouped_gemm(false, EPI_RESID_ADD, dn, s);
-    }
-    if (e == hipSuccess)
-        e = launch_norm_gate(T, D, E, rms_eps, x, w_router, bias, feat, expert_ids, logits, s);
-    return st_of(e);
+size_t readme_router_tf_cached_workspace_bytes(int64_t T, int32_t R, int64_t D, int64_t F,
+                                               int64_t max_blocks) {
+    const size_t n = readme_router_tf_workspace_bytes(T, D, F);
+    const int32_t H = (int32_t)(D / kHeadDim);
+    const size_t at = n ? readme_attention_kv_workspace_bytes(T, R, H, H, kHeadDim, max_blocks) : 0;
+    return at ? n + at : 0;
+}
+
+readme_status readme_router_tf_cached(readme_kv_type kt, int64_t T, int32_t R, int64_t D, int64_t F,
+                                      int32_t E, int64_t V, const int32_t* tokens,
+                                      const int32_t* req_offsets, const int32_t* lens,
+                                      const int32_t* table, int64_t max_blocks, int64_t n_blocks,
+                                      void* codes, float* scales, const void* emb,
+                                      const void* packed, const void* w_router, const float* bias,
+                                      float rms_eps, int32_t* expert_ids, float* logits,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+    readme_status st = check_block(D, F);
+    if (st != README_OK) return st;
+    if (T < 0 || R < 0 || V < 1 || !(rms_eps >= 0.0f)) return README_ERR_ARG;
+    if (E < 1 || E > README_MAX_EXPERTS || T > INT32_MAX) return README_ERR_UNSUPPORTED;
+    const int32_t H = (int32_t)(D / kHeadDim);
+    bool done;
+    st = kv_check_attention(kt, T, R, H, H, kHeadDim, max_blocks, n_blocks, &done);
+    if (st != README_OK || done) return st;
+    if (R < 1 || !tokens || !req_offsets || !emb || !packed || !w_router || !expert_ids ||
+        !workspace)
+        return README_ERR_ARG;
+    if (!al16(emb) || !al16(packed) || !al16(w_router) || !al16(workspace)) return README_ERR_ARG;
+    const KvCacheArgs c = kv_cache_args(T, R, H, kHeadDim, req_offsets, lens, table, max_blocks,
+                                        n_blocks, codes, scales);
+    if ((st = kv_check_cache(c)) != README_OK) return st;
+    if (workspace_bytes < readme_router_tf_cached_workspace_bytes(T, R, D, F, max_blocks))
+        return README_ERR_WORKSPACE;
+
+    return st_of(run_block(T, R, D, F, E, V, tokens, req_offsets, &c, kt, emb, packed, w_router, bias,
+                           rms_eps, expert_ids, logits, workspace, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -127,3 +127,39 @@ def test_python_form_refuses():
         L.readme_kv_write(0, k, k, i(2), i(1), i(1, 3), codes, scales)
     with pytest.raises(ValueError, match="device tensors"):
         L.readme_attention_kv(0, k, i(2), i(1), i(1, 3), codes, scales, H=2)
+
+
+def _router(lib, **k):
+    g = lambda n, d: k.get(n, d)  # noqa: E731
+    return lib.readme_router_tf_cached(
+        g("kt", 0), g("T", 16), g("R", 2), g("D", 256), g("F", 64), g("E", 8), g("V", 100),
+        g("tokens", FAKE), g("offsets", FAKE), g("lens", FAKE), g("table", FAKE), g("mb", 4),
+        g("nb", 9), g("codes", FAKE), g("scales", FAKE), g("emb", FAKE), g("packed", FAKE),
+        g("w_router", FAKE), None, ctypes.c_float(g("eps", 1e-5)), g("ids", FAKE), None,
+        g("ws", FAKE), g("wsb", 1 << 40), None)
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(T=-1), 1), (dict(R=-1), 1), (dict(R=0), 1), (dict(mb=0), 1), (dict(nb=0), 1),
+    (dict(kt=2), 2), (dict(D=0), 1), (dict(D=192), 2), (dict(D=32768), 2), (dict(F=0), 1),
+    (dict(E=0), 2), (dict(E=257), 2), (dict(V=0), 1), (dict(eps=-1.0), 1),
+    (dict(T=1 << 27), 2), (dict(R=(1 << 22) + 1), 2), (dict(mb=1 << 26), 2), (dict(nb=1 << 32), 2),
+    (dict(tokens=None), 1), (dict(offsets=None), 1), (dict(lens=None), 1), (dict(table=None), 1),
+    (dict(codes=None), 1), (dict(scales=None), 1), (dict(emb=None), 1), (dict(packed=None), 1),
+    (dict(w_router=None), 1), (dict(ids=None), 1), (dict(ws=None), 1), (dict(ws=ODD), 1),
+    (dict(codes=ODD), 1), (dict(emb=ODD), 1), (dict(wsb=64), 3),
+])
+def test_cached_router_refuses(lib, bad, status):
+    assert _router(lib, **bad) == status
+
+
+def test_cached_router_workspace(lib):
+    w = lib.readme_router_tf_cached_workspace_bytes
+    need = w(16, 2, 256, 64, 4)
+    assert need == (lib.readme_router_tf_workspace_bytes(16, 256, 64) +
+                    lib.readme_attention_kv_workspace_bytes(16, 2, 2, 2, 128, 4))
+    assert _router(lib, wsb=need - 1) == 3
+    assert w(16, 2, 192, 64, 4) == 0 and w(16, 0, 256, 64, 4) == 0 and w(-1, 2, 256, 64, 4) == 0
+    none = dict(T=0, R=0, mb=0, nb=0, tokens=None, offsets=None, lens=None, table=None, codes=None,
+                scales=None, emb=None, packed=None, w_router=None, ids=None, ws=None, wsb=0)
+    assert _router(lib, **none) == 0
