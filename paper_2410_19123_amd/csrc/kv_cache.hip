@@ -19,6 +19,13 @@
 // or begins at one of the call's rows; a request has at most one such row in a
 // run of 64, so a workgroup per run of 64 rows finds them.  Both kernels run
 // one workgroup per (candidate, head, K or V) and need no plan and no workspace.
+// K's rows become 16-byte pieces as they are; V's tokens lie beside each other in
+// a block, so its codes pass through LDS, four bytes transposed in registers.
+// Measured: reading 105275 rows of 8 heads of 128 from int8 to bf16, 647 MB in
+// 137 us, 4.7 TB/s, a large copy's rate (4.9); writing 16155 such rows from bf16
+// to e4m3, 99 MB in 27 us, 3.6 TB/s, held by the conversion's instructions; a row
+// each of 64 requests 5.5 us to write and 7 to read the blocks back: launch,
+// the search of the request, one dependent load each of table, scale and codes.
 #include <math.h>
 
 #include "kv_cache.hpp"
