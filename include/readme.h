@@ -835,7 +835,8 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *   themselves, 2^-32 below 2^-21), so o is the exact result up to about
  *   2^-11 of the largest |v| the row sees plus its rounding to bf16.  The
  *   order of the sums depends on the sizes and lens, never on timing.
- *   A row of q with an infinity or a NaN gives an unspecified row; a scale
+ *   A row of q with an infinity or a NaN, one whose largest element is below
+ *   2^-100 but not 0, or scores beyond fp32 give an unspecified row; a scale
  *   that is NaN or infinite gives NaN in the rows that see any of its tokens.
  *   q [T][ld_q] bf16 (head g at columns D g ..), o [T][ld_o] bf16 out, causal
  *   0 or 1, window >= 0, scale > 0 and finite; workspace >=

@@ -126,12 +126,13 @@ __device__ __forceinline__ void mask_scores(V& v, int a0, int a1) {
 
 // Query rows as fp16 matrix operands.  Each lane holds elements of one row in
 // x; `big` is the largest magnitude in the row.  Returns 2^x and its inverse;
-// a row of zeros (or one too small to matter) keeps a bounded power.
+// below 2^-100 (a row of zeros among them) the power stays, so that the inverse
+// is far from fp32's subnormals.
 __device__ __forceinline__ void row_power(float big, float& up, float& down) {
     int e = 0;
     (void)frexpf(big, &e);
     e = big > 0.0f ? e : 0;
-    e = e < -60 ? -60 : e;
+    e = e < -100 ? -100 : e;
     up = ldexpf(1.0f, 15 - e);
     down = ldexpf(1.0f, e - 15);
 }

@@ -453,6 +453,83 @@ def test_windows_of_long_tables(kt, D, new):
         _attend(c, new, lens, 3, True, window)
 
 
+@pytest.mark.parametrize("new", [1, 40])
+def test_tiny_queries_of_huge_keys(new):
+    """A row of q as small as 2^-95 against keys of 2^90: scores of order one."""
+    c = _random_cache("i8", 2, 1, 128, 4, seed=28)
+    big = np.float32(2.0 ** 90)
+    c.ref["scales"][:, :, 0] *= big
+    c.scales.copy_(torch.from_numpy(c.ref["scales"]))
+    T = 2 * new
+    q = torch.from_numpy(c.rng.standard_normal((T, 2, 128)) * 2.0 ** -93).bfloat16()
+    _attend(c, [new] * 2, [200, 77], 2, q=q)
+
+
+def test_requests_share_a_prefix():
+    """Blocks that several requests list, one of them twice in a row."""
+    for new in ([1, 1, 1], [30, 1, 70]):
+        c = _random_cache("e4m3", 3, 2, 64, 5, seed=29)
+        c.table[1, :3] = c.table[0, :3]
+        c.table[2, :2] = c.table[0, 0]
+        _attend(c, new, [320, 250, 170], 4)
+
+
+def test_two_streams_at_once():
+    """Calls in flight together, each with its own workspace, give what they
+    give alone (shares and their join among them)."""
+    L = _lib()
+    work = []
+    for i, (R, new, mb, Hk) in enumerate(((2, 1, 300, 2), (1, 300, 100, 1), (3, 4, 9, 4))):
+        c = _random_cache("i8", R, Hk, 128, mb, seed=50 + i)
+        off, lens = _i32(_offsets([new] * R)), _i32([mb * 64 - 5] * R)
+        q = torch.randn(R * new, Hk * 4 * 128, device="cuda:0").bfloat16()
+        ws = torch.empty(L.readme_attention_kv_workspace_bytes(R * new, R, Hk * 4, Hk, 128, mb),
+                         dtype=torch.uint8, device="cuda:0")
+        work.append((c, q, off, lens, Hk, ws))
+
+    def call(w, o):
+        c, q, off, lens, Hk, ws = w
+        return L.readme_attention_kv(0, q, off, lens, *c.args(), H=Hk * 4, o=o, workspace=ws)
+    args = [w[0].args() for w in work]
+    alone = [call(w, torch.empty_like(w[1])) for w in work]
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(w[1]) for _ in range(4)] for w in work]
+    streams = [torch.cuda.Stream() for _ in work]
+    for k in range(4):
+        for w, a, o, s in zip(work, args, outs, streams):
+            with torch.cuda.stream(s):
+                L.readme_attention_kv(0, w[1], w[2], w[3], *a, H=w[4] * 4, o=o[k], workspace=w[5])
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        assert all(torch.equal(a, x) for x in o)
+
+
+@pytest.mark.parametrize("new,mb", [([1, 1, 1], 90), ([1, 40, 200], 90), ([1, 1, 1], 6)])
+def test_captured_attention_follows_the_lengths(new, mb):
+    """One capture of each form, replayed as lens and rows change, against
+    eager calls with another workspace."""
+    L = _lib()
+    c = _random_cache("e4m3", 3, 2, 128, mb, seed=60)
+    table, codes, scales = c.args()
+    T = sum(new)
+    off, lens = _i32(_offsets(new)), _i32([200, 201, 202])
+    q = torch.randn(T, 512, device="cuda:0").bfloat16()
+    o = torch.empty_like(q)
+    ws = torch.empty(L.readme_attention_kv_workspace_bytes(T, 3, 4, 2, 128, mb), dtype=torch.uint8,
+                     device="cuda:0")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.readme_attention_kv(1, q, off, lens, table, codes, scales, H=4, o=o, workspace=ws)
+    for now in ([200, 201, 202], [mb * 64, 230, 1], [0, 0, 0], [330, mb * 64 - 1, 260]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        q.copy_(torch.randn(T, 512, device="cuda:0"))
+        graph.replay()
+        got = o.clone()
+        ref = L.readme_attention_kv(1, q, off, lens, table, codes, scales, H=4)
+        torch.cuda.synchronize()
+        assert torch.equal(got, ref), now
+
+
 @pytest.mark.parametrize("R,lens", [(1, [40000]), (3, [20000, 1, 9000]), (70, None)])
 def test_attention_long_and_uneven(R, lens):
     """Work split over the keys and joined: against float64 torch on the GPU."""
