@@ -18,9 +18,8 @@ __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int6
     constexpr int kPart = kv_part_floats<D, ROWS>;
     constexpr int kStep = 1024 / D;
     const int h = blockIdx.y;
-    int64_t tl;
-    const int64_t r = kv_slot_request<ROWS>(a, blockIdx.x, tl);
-    const KvRequest q = kv_request(a, r);
+    int64_t r, tl;
+    const KvRequest q = kv_slot_request<ROWS>(a, blockIdx.x, r, tl);
     const KvPlan p = kv_plan<ROWS>(a, q);
     const int i = (int)blockIdx.z * kStep + threadIdx.x / (D / 4);
     const int64_t row = tl * ROWS + i;

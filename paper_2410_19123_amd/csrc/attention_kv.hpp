@@ -146,14 +146,15 @@ struct KvRequest {
     int block1;
 };
 
-__device__ __forceinline__ KvRequest kv_request(const KvAttnArgs& a, int64_t r) {
+// Request with rows offsets off0 .. off1 and `len` tokens.
+__device__ __forceinline__ KvRequest kv_request_of(const KvAttnArgs& a, int64_t off0, int64_t off1,
+                                                   int64_t len) {
     KvRequest q;
     int64_t lo, hi;
-    kv_rows(a.c.offsets, a.c.T, r, lo, hi);
+    kv_clamp_rows(off0, off1, a.c.T, lo, hi);
     q.row0 = lo;
     q.n = (int)(hi - lo);
     const int64_t cap = a.c.max_blocks * kKvBlock;
-    int64_t len = a.c.lens[r];
     const int64_t first = len - q.n;
     int64_t b1 = len < cap ? len : cap;
     b1 = b1 < 0 ? 0 : (b1 + kKvBlock - 1) / kKvBlock;
@@ -163,6 +164,9 @@ __device__ __forceinline__ KvRequest kv_request(const KvAttnArgs& a, int64_t r) 
     q.block1 = (int)b1;
     q.block0 = (int)(b0 < b1 ? b0 : b1);
     return q;
+}
+__device__ __forceinline__ KvRequest kv_request(const KvAttnArgs& a, int64_t r) {
+    return kv_request_of(a, a.c.offsets[r], a.c.offsets[r + 1], a.c.lens[r]);
 }
 
 // Keys [lo, hi) that a row at position p sees.
@@ -353,12 +357,14 @@ struct KvWalk {
 
 // Tile j of request r is slot floor(offsets[r] G / ROWS) + r + j, which needs no
 // sum over the requests (and leaves some slots empty): the request of a slot,
-// and the tile.
+// and the tile.  The last step of the search has one request a lane and loads all
+// of it, one dependent load less.
 template <int ROWS>
-__device__ __forceinline__ int64_t kv_slot_request(const KvAttnArgs& a, int64_t slot, int64_t& tile) {
+__device__ __forceinline__ KvRequest kv_slot_request(const KvAttnArgs& a, int64_t slot, int64_t& r,
+                                                     int64_t& tile) {
     const int lane = threadIdx.x & 63;
     int64_t lo = 0, n = a.c.R;
-    while (n > 1) {
+    while (n > 64) {
         const int64_t step = (n + 63) / 64, i = lane * step;
         const bool le = i < n && (int64_t)a.c.offsets[lo + i] * a.G / ROWS + lo + i <= slot;
         const int below = __popcll(__ballot(le));
@@ -366,8 +372,20 @@ __device__ __forceinline__ int64_t kv_slot_request(const KvAttnArgs& a, int64_t 
         lo += skip;
         n = n - skip < step ? n - skip : step;
     }
-    tile = slot - ((int64_t)a.c.offsets[lo] * a.G / ROWS + lo);
-    return lo;
+    int off0 = 0, off1 = 0, len = 0;
+    if (lane < n) {
+        off0 = a.c.offsets[lo + lane];
+        off1 = a.c.offsets[lo + lane + 1];
+        len = a.c.lens[lo + lane];
+    }
+    const bool le = lane < n && (int64_t)off0 * a.G / ROWS + lo + lane <= slot;
+    const int below = __popcll(__ballot(le)), l = below > 0 ? below - 1 : 0;
+    off0 = __builtin_amdgcn_readlane(off0, l);
+    off1 = __builtin_amdgcn_readlane(off1, l);
+    len = __builtin_amdgcn_readlane(len, l);
+    r = lo + l;
+    tile = slot - ((int64_t)off0 * a.G / ROWS + r);
+    return kv_request_of(a, off0, off1, len);
 }
 __host__ __device__ inline int64_t kv_slots(int64_t T, int64_t R, int64_t G, int rows) { return T * G / rows + R; }
 

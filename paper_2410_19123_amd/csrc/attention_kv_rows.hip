@@ -325,10 +325,9 @@ void k_attention_rows(KvAttnArgs a, int64_t* __restrict__ plan, float* __restric
     const int wv = threadIdx.x >> 6;
     RowsState<KT, D> st;
     if constexpr (!SHARES) {
-        int64_t tile;
+        int64_t r, tile;
         const int h = (int)(blockIdx.x % a.c.Hk);
-        const int64_t r = kv_slot_request<kRows>(a, blockIdx.x / a.c.Hk, tile);
-        const KvRequest q = kv_request(a, r);
+        const KvRequest q = kv_slot_request<kRows>(a, blockIdx.x / a.c.Hk, r, tile);
         if (tile < 0 || tile * kRows >= (int64_t)q.n * a.G) return;
         st.walk(a, q, tile, r, h, q.block0, q.block1 - q.block0, wv, W);
         join_waves<KT, D, W>(a, q, tile, h, st, xs, nullptr);

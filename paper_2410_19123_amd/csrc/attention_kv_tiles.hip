@@ -343,9 +343,8 @@ void k_attention_tiles(KvAttnArgs a, int64_t* __restrict__ plan, float* __restri
         const int h = (int)(blockIdx.x % a.c.Hk);
         const int64_t slot = (x % a.c.R) * len + (len - 1 - x / a.c.R);
         if (slot >= S) return;
-        int64_t tile;
-        const int64_t r = kv_slot_request<kTilesTile>(a, slot, tile);
-        const KvRequest q = kv_request(a, r);
+        int64_t r, tile;
+        const KvRequest q = kv_slot_request<kTilesTile>(a, slot, r, tile);
         if (tile < 0 || tile * kTilesTile >= (int64_t)q.n * a.G) return;
         st.start(a, q, tile, h);
         // Blocks that any of the tile's rows sees: its first and last row's

@@ -46,11 +46,14 @@ __device__ __forceinline__ int64_t kv_block_of(const int32_t* __restrict__ table
 }
 
 // Rows [lo, hi) of request r, kept inside [0, T] whatever the offsets hold.
-__device__ __forceinline__ void kv_rows(const int32_t* __restrict__ offsets, int64_t T, int64_t r,
-                                        int64_t& lo, int64_t& hi) {
-    const int64_t a = offsets[r], b = offsets[r + 1];
+__device__ __forceinline__ void kv_clamp_rows(int64_t a, int64_t b, int64_t T, int64_t& lo,
+                                              int64_t& hi) {
     lo = a < 0 ? 0 : (a > T ? T : a);
     hi = b < lo ? lo : (b > T ? T : b);
+}
+__device__ __forceinline__ void kv_rows(const int32_t* __restrict__ offsets, int64_t T, int64_t r,
+                                        int64_t& lo, int64_t& hi) {
+    kv_clamp_rows(offsets[r], offsets[r + 1], T, lo, hi);
 }
 
 // The last request r with offsets[r] <= t (0 if none), found by the 64 lanes
