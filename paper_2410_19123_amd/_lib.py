@@ -825,17 +825,19 @@ def _kv_cache_args(offsets, lens, table, codes, scales):
     return where[0], size[1], size[3] // README_KV_BLOCK, where[1], size[0], dev
 
 
-# The current stream's handle without building a torch.cuda.Stream for it.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# The current stream's handle and device without torch.cuda's objects and checks
+# (there are CUDA tensors by now), where this torch has them.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _kv_call(dev: int, name: str, *args) -> None:
     """The call on device `dev` (made current for it) and its current stream."""
-    if torch.cuda.current_device() != dev:
+    if _raw_device() != dev:
         with torch.cuda.device(dev):
             return _kv_call(dev, name, *args)
-    st = getattr(load(), name)(*args, _raw_stream(dev) if _raw_stream is not None else
-                               torch.cuda.current_stream(dev).cuda_stream)
+    st = getattr(load(), name)(*args, _raw_stream(dev))
     if st != 0:
         raise ReadmeError(name, st)
 

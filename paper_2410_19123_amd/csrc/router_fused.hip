@@ -111,7 +111,8 @@ __device__ __forceinline__ void put_group(const float (&v)[16], int grp, int l32
     }
 }
 
-// Embedding, norm, q|k|v, RoPE.
+// Embedding, norm, q|k|v, RoPE.  GIVEN: the positions are in `pos` already.
+template <bool GIVEN>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void k_router_head(int64_t T, int32_t R, int64_t V, float eps, const int32_t* __restrict__ tokens,
                    const int32_t* __restrict__ ro, const uint16_t* __restrict__ emb,
@@ -136,7 +137,7 @@ void k_router_head(int64_t T, int32_t R, int64_t V, float eps, const int32_t* __
         const int64_t t = t0 + wave * 4 + j;
         tok[j] = t < T ? (int64_t)tokens[t] : -1;
     }
-    const bool staged = R + 1 <= kRoLds;
+    const bool staged = !GIVEN && R + 1 <= kRoLds;
     if (staged)
         for (int i = tid; i <= R; i += NW * 64) ro_lds[i] = ro[i];
 #pragma unroll
@@ -159,8 +160,13 @@ void k_router_head(int64_t T, int32_t R, int64_t V, float eps, const int32_t* __
     __syncthreads();
     if (lane < 4) {
         const int64_t t = t0 + wave * 4 + lane;
-        const int32_t p = t < T ? position_of(t, R, staged ? ro_lds : ro) : 0;
-        if (t < T) pos[t] = p;
+        int32_t p = 0;
+        if constexpr (GIVEN) {
+            if (t < T) p = pos[t];
+        } else {
+            p = t < T ? position_of(t, R, staged ? ro_lds : ro) : 0;
+            if (t < T) pos[t] = p;
+        }
         pos_lds[wave * 4 + lane] = p;
     }
     if (tid < 64) inv[tid] = pow(10000.0, -2.0 * (double)tid / 128.0);
@@ -432,9 +438,10 @@ void k_router_tail(int64_t T, int Fp, int E, float eps, const uint16_t* __restri
 
 hipError_t launch_router_head(int64_t T, int32_t R, int64_t V, float eps, const int32_t* tokens,
                               const int32_t* ro, const void* emb, float* x, uint16_t* a,
-                              int32_t* pos, int32_t* offs, const void* wqkv, uint16_t* qkv,
-                              hipStream_t s) {
-    k_router_head<<<(unsigned)ceil_div(T, TOK), NW * 64, 0, s>>>(
+                              int32_t* pos, bool given, int32_t* offs, const void* wqkv,
+                              uint16_t* qkv, hipStream_t s) {
+    const auto head = given ? k_router_head<true> : k_router_head<false>;
+    head<<<(unsigned)ceil_div(T, TOK), NW * 64, 0, s>>>(
         T, R, V, eps, tokens, ro, reinterpret_cast<const uint16_t*>(emb), x, a, pos, offs,
         reinterpret_cast<const char*>(wqkv), qkv);
     return hipGetLastError();

@@ -775,12 +775,34 @@ hipError_t run_block(int64_t T, int32_t R, int64_t D, int64_t F, int32_t E, int6
 
     const bool wide = T * D >= (int64_t)4 << 20 && D <= 1024;
     const void* mlp = pk + 4 * D * D * 2;
-    if (!cache && D == kFusedRouterWidth && padded_I(F) <= kFusedRouterMlp &&
-        T >= fused_router_tokens(F) && get_gemm_tile() == 0) {
-        hipError_t e = launch_router_head(T, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
-                                          offs, pk, qkv, s);
+    auto cache_positions = [&] {
+        k_cache_positions<<<(unsigned)R, 256, 0, s>>>(T, req_offsets, cache->lens, pos);
+        return hipGetLastError();
+    };
+    auto attention = [&] {
+        if (!cache) return launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
+        const hipError_t e =
+            launch_kv_write(kt, README_BF16, *cache, qkv + D, 3 * D, qkv + 2 * D, 3 * D, s);
+        if (e != hipSuccess) return e;
+        KvAttnArgs kva{};
+        kva.c = *cache;
+        kva.q = qkv;
+        kva.ld_q = 3 * D;
+        kva.o = o;
+        kva.ld_o = D;
+        kva.G = 1;
+        kva.score = 1.4426950408889634f / sqrtf((float)kHeadDim);
+        kva.causal = 1;
+        kva.ws = at(README_RTF_END);
+        return launch_kv_attention(kt, kva, s);
+    };
+    if (D == kFusedRouterWidth && padded_I(F) <= kFusedRouterMlp && T >= fused_router_tokens(F) &&
+        get_gemm_tile() == 0) {
+        hipError_t e = cache ? cache_positions() : hipSuccess;
         if (e == hipSuccess)
-            e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
+            e = launch_router_head(T, R, V, rms_eps, tokens, req_offsets, emb, x, a, pos,
+                                   cache != nullptr, offs, pk, qkv, s);
+        if (e == hipSuccess) e = attention();
         if (e == hipSuccess)
             e = launch_router_tail(T, F, E, rms_eps, o, pk + 3 * D * D * 2, mlp, w_router, bias, x,
                                    m, h, feat, expert_ids, logits, s);
@@ -793,27 +815,9 @@ hipError_t run_block(int64_t T, int32_t R, int64_t D, int64_t F, int32_t E, int6
         g.tile = wide ? kTileQkv : 0;
         e = launch_grouped_gemm(false, EPI_STORE, g, s);
     }
-    if (e == hipSuccess && cache) {
-        k_cache_positions<<<(unsigned)R, 256, 0, s>>>(T, req_offsets, cache->lens, pos);
-        e = hipGetLastError();
-    }
+    if (e == hipSuccess && cache) e = cache_positions();
     if (e == hipSuccess) e = launch_rope(T, 2 * H, pos, qkv, 3 * D, s);
-    if (e == hipSuccess && cache) {
-        e = launch_kv_write(kt, README_BF16, *cache, qkv + D, 3 * D, qkv + 2 * D, 3 * D, s);
-        KvAttnArgs kva{};
-        kva.c = *cache;
-        kva.q = qkv;
-        kva.ld_q = 3 * D;
-        kva.o = o;
-        kva.ld_o = D;
-        kva.G = 1;
-        kva.score = 1.4426950408889634f / sqrtf((float)kHeadDim);
-        kva.causal = 1;
-        kva.ws = at(README_RTF_END);
-        if (e == hipSuccess) e = launch_kv_attention(kt, kva, s);
-    } else if (e == hipSuccess) {
-        e = launch_attention(T, H, R, pos, qkv, qkv + D, qkv + 2 * D, 3 * D, o, D, s);
-    }
+    if (e == hipSuccess) e = attention();
     if (e == hipSuccess) {
         GemmArgs g = plain_args(o, D, pk + 3 * D * D * 2, D, offs, T, x, D);
         g.tile = wide ? kTileNarrow : 0;
