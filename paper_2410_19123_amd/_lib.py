@@ -932,6 +932,10 @@ def readme_router_tf_cached(kt: int, tokens, req_offsets, lens, table, codes, sc
         raise ValueError("bias must be fp32 [E]")
     if expert_ids is None:
         expert_ids = torch.empty(T, dtype=torch.int32, device=codes.device)
+    if expert_ids.dtype != torch.int32 or expert_ids.numel() < T:
+        raise ValueError("expert_ids must be int32 [T]")
+    if logits is not None and (logits.dtype != torch.float32 or logits.shape != (T, E)):
+        raise ValueError("logits must be fp32 [T][E]")
     if workspace is None:
         ws = readme_router_tf_cached_workspace_bytes(T, R, D, F, mb)
         workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=codes.device)
