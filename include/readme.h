@@ -846,10 +846,9 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *
  * All require D of 64, 128 or 256, 1 <= Hk <= 65535, H a multiple of Hk,
  * R <= 2^22, T H / Hk <= 2^27 (for the attention also T H / 16 + R Hk <= 2^23),
- * row strides at least the row's width and 16-byte
- * multiples, arrays of rows 16-byte aligned; T = 0 enqueues nothing, else
- * R >= 1, max_blocks >= 1 and n_blocks >= 1.  The size queries return 0 for
- * arguments outside that set.
+ * row strides at least the row's width and 16-byte multiples, arrays of rows
+ * 16-byte aligned; T = 0 enqueues nothing, else R >= 1, max_blocks >= 1 and
+ * n_blocks >= 1.  The size queries return 0 for arguments outside that set.
  */
 size_t readme_kv_codes_bytes(int64_t n_blocks, int32_t Hk, int32_t D);
 size_t readme_kv_scales_bytes(int64_t n_blocks, int32_t Hk);
