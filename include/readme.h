@@ -832,9 +832,11 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *   token is zeros.  Scores, running softmax and sums in fp32; a row of q
  *   enters scaled by a power of two in fp16, exactly down to 2^-28 of its
  *   largest element, the codes exactly, the weights rounded to fp16 (2^-11 of
- *   themselves, 2^-32 below 2^-21), so o is the exact result up to about
- *   2^-11 of the largest |v| the row sees plus its rounding to bf16.  The
- *   order of the sums depends on the sizes and lens, never on timing.
+ *   themselves; below 2^-21 by 2^-32, or by up to 2^-24 in blocks of a smaller
+ *   value scale than others that the row sees), so o is the exact result up to
+ *   about 2^-11 of the largest |v| the row sees plus its rounding to bf16,
+ *   unless a block that it sees has a value scale above 2^100 times that |v|.
+ *   The order of the sums depends on the sizes and lens, never on timing.
  *   A row of q with an infinity or a NaN, one whose largest element is below
  *   2^-100 but not 0, or scores beyond fp32 give an unspecified row; a scale
  *   that is NaN or infinite gives NaN in the rows that see any of its tokens.

@@ -14,14 +14,18 @@
 //   m is raised, and the sums rescaled, only when a block's maximum passes it by
 //   more than kLazy, so weights reach 2^kLazy at most and most blocks skip the
 //   rescaling.
-//   Values: the block's vs goes into the exponent as r = vs / vref, vref the
-//   largest scale so far (the accumulators are in units of vref), so it costs
-//   nothing per weight: p = 2^(score - m + log2 r + kUp) in fp16 times the codes,
-//   added in fp32; l adds (sum of the block's p in fp32) / r.  p rounds to 11 bits
-//   (at most 2^-11 of itself; against bf16 weights, 8 bits, an eighth of the error for
-//   the same instructions), and kUp keeps weights down to 2^-21 out of fp16's
-//   subnormals; smaller ones are off by at most 2^-32.  o is therefore within
-//   about 2^-11 max|v| of the exact result before its own rounding to bf16.
+//   Values: the block's vs goes into the exponent as r = vs / vref (the
+//   accumulators are in units of vref), so it costs nothing per weight:
+//   p = 2^(score - m + log2 r + kUp) in fp16 times the codes, added in fp32; l adds
+//   (sum of the block's p in fp32) / r.  p rounds to 11 bits (at most 2^-11 of itself;
+//   against bf16 weights, 8 bits, an eighth of the error for the same instructions),
+//   and kUp keeps weights down to 2^-21 out of fp16's subnormals; smaller ones are off
+//   by at most 2^-32, over r.
+//   vref is of a row, and of blocks that it sees some token of: raised to a larger
+//   vs, lowered to one below 2^-8 vref (value_unit), so r is in [2^-8, 1] however far
+//   apart scales lie, and however small the codes that came with the large ones.
+//   o is therefore within about 2^-11 max|v| of the exact result before its own
+//   rounding to bf16.
 #pragma once
 
 #include "kv_cache.hpp"
@@ -92,12 +96,55 @@ __device__ __forceinline__ uint2 pack_bf16(float a, float b, float c, float d) {
                       __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2v)));
 }
 
-// A block's value scale against the running largest, log_vref = log2 vref:
-// log2 r and 1 / r.  Below 2^-40 the block's values are under fp32's rounding of
-// the rest and r stays there.
+// A block's value scale against the row's unit, log_vref = log2 vref: log2 r and
+// 1 / r.  At 2^-40 and below every p rounds to zero in fp16: a scale of zero, or one
+// that value_unit left that far under the sums.
 __device__ __forceinline__ void value_ratio(float vs, float log_vref, float& log_r, float& inv_r) {
     log_r = fmaxf(__builtin_amdgcn_logf(vs) - log_vref, -40.0f);
     inv_r = __builtin_amdgcn_exp2f(-log_r);
+}
+
+// The lane's row sees any token of the block at j0.
+__device__ __forceinline__ bool sees_block(int lo, int hi, int j0) {
+    return max(lo, j0) < min(hi, j0 + kKvBlock);
+}
+
+// The unit of a row's sums, for a block of value scale vs.  Lowering multiplies the
+// sums, which may hold what a larger scale left: they stop at 2^100 units, and what
+// the block adds to sums that large, at most 2^53, is under fp32's rounding of them.
+// A unit raised by more than 2^100 may lose them.  A NaN moves nothing.  `row_max`:
+// the largest over the lanes that share the row.
+constexpr float kUnitLow = 0x1p-8f;
+template <class A, int N, class F>
+__device__ __forceinline__ void value_unit(float vs, bool sees, float& vref, float& log_vref, A (&acc)[N],
+                                           F&& row_max) {
+    const bool up = sees && vs > vref, down = sees && vs > 0.0f && vs < vref * kUnitLow;
+    if (!__any(up || down)) return;
+    const float ratio = vref * __builtin_amdgcn_rcpf(vs);
+    float f = 1.0f, u = vref;
+    if (up) {
+        f = fminf(ratio, 1.0f);  // at first 0 / vs
+        u = vs;
+    }
+    if (__any(down)) {
+        float big = 0.0f;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(A) / sizeof(float)); ++k) big = fmaxf(big, fabsf(acc[d][k]));
+        big = row_max(big);
+        if (down) {
+            const float most = fminf(0x1p100f * __builtin_amdgcn_rcpf(big), 0x1p126f);
+            f = big == 0.0f ? 1.0f : fminf(ratio, most);
+            u = big == 0.0f || ratio <= most ? vs : vref * __builtin_amdgcn_rcpf(most);
+        }
+    }
+    if (up || down) {  // elsewhere vref may be 0 still, with the logarithm 0
+        vref = u;
+        log_vref = __builtin_amdgcn_logf(u);
+    }
+#pragma unroll
+    for (int d = 0; d < N; ++d) acc[d] *= f;
 }
 
 // The scores' factor and offset of a row: 2^(factor * sum + offset) is a weight.
@@ -113,7 +160,7 @@ __device__ __forceinline__ float score_offset(float log_r, float m) {
 // other rows' weights for it are 0).
 __device__ __forceinline__ bool bad_scales(float ks, float vs) { return !(ks < INFINITY && vs < INFINITY); }
 __device__ __forceinline__ float bad_sum(float l, int lo, int hi, int j0) {
-    return max(lo, j0) < min(hi, j0 + kKvBlock) ? __builtin_nanf("") : l;
+    return sees_block(lo, hi, j0) ? __builtin_nanf("") : l;
 }
 
 // Token k of a lane's 16 is seen if a0 <= k < a1.
@@ -401,8 +448,8 @@ __device__ __forceinline__ KvBlockRef kv_block_ref(const KvAttnArgs& a, int64_t 
     if (b.blk >= 0) {
         const float2 sc =
             *reinterpret_cast<const float2*>(a.c.scales + ((int64_t)b.blk * a.c.Hk + h) * 2);
-        // An infinite scale counts as NaN: as the largest value scale so far it
-        // would empty the sums of rows that do not see its block.
+        // An infinite scale counts as NaN: its logarithm and products of a score
+        // of zero are not numbers.
         const bool bad = bad_scales(sc.x, sc.y);
         b.ks = bad ? __builtin_nanf("") : sc.x;
         b.vs = bad ? __builtin_nanf("") : sc.y;

@@ -144,14 +144,11 @@ struct RowsState {
         }
         load_k(next);
 
-        // Units of the sums: the largest value scale so far.
-        if (vs > vref) {
-            const float f = vref * __builtin_amdgcn_rcpf(vs);
-            vref = vs;
-            log_vref = __builtin_amdgcn_logf(vs);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) acc[d] *= f;
-        }
+        const bool edge = j0 + kKvBlock > min_hi || j0 < max_lo;
+        value_unit(vs, !edge || sees_block(lo, hi, j0), vref, log_vref, acc, [](float x) {
+            x = fmaxf(x, __shfl_xor(x, 16, 64));
+            return fmaxf(x, __shfl_xor(x, 32, 64));
+        });
         float log_r, inv_r;
         value_ratio(vs, log_vref, log_r, inv_r);
 
@@ -161,7 +158,7 @@ struct RowsState {
 #pragma unroll
         for (int k = 0; k < 16; ++k) z[k] = s[k >> 2][k & 3];
         const int a0 = lo - j0 - 16 * qt, a1 = hi - j0 - 16 * qt;
-        if (j0 + kKvBlock > min_hi || j0 < max_lo) mask_scores(z, a0, a1);
+        if (edge) mask_scores(z, a0, a1);
         float mx = -INFINITY;
 #pragma unroll
         for (int k = 0; k < 16; ++k) mx = fmaxf(mx, z[k]);

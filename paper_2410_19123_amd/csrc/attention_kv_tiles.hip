@@ -144,19 +144,15 @@ struct TileState {
         f16x8 vf[4 * ND];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) vf[i] = v_at(i);
-        if (vs > vref) {
-            const float f = vref * __builtin_amdgcn_rcpf(vs);
-            vref = vs;
-            log_vref = __builtin_amdgcn_logf(vs);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) acc[d] *= f;
-        }
+        const bool edge = j0 + kKvBlock > min_hi || j0 < max_lo;
+        value_unit(vs, !edge || sees_block(lo, hi, j0), vref, log_vref, acc,
+                   [](float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); });
         float log_r, inv_r;
         value_ratio(vs, log_vref, log_r, inv_r);
         const float c = score_factor(cq, ks);
         // score (g, k) is token j0 + 32 g + 16 hf + k
         const int a0 = lo - j0 - 16 * hf, a1 = hi - j0 - 16 * hf;
-        if (j0 + kKvBlock > min_hi || j0 < max_lo) {
+        if (edge) {
             mask_scores(s[0], a0, a1);
             mask_scores(s[1], a0 - 32, a1 - 32);
         }
