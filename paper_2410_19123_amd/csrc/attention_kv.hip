@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int6
     const int64_t row = tl * ROWS + i;
     if (tl < 0 || row >= (int64_t)q.n * a.G) return;
     const int d = threadIdx.x % (D / 4) * 4;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f, unit = 0.0f;
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     if (p.blocks > 0) {
         const int64_t share = plan[0];
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int6
         // Workgroup g's part is its second where the pair's first block is in
         // its share.
         for (int64_t g = g0; g <= g1; g += 4) {
-            float pm[4], pl[4];
+            float pm[4], pl[4], pu[4];
             f32x4 pa[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -43,28 +43,33 @@ __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int6
                 const float* pp = parts + (gk * 2 + (gk == g0 ? 1 : 0)) * kPart;
                 pm[k] = g + k <= g1 ? pp[ROWS * D + i] : -INFINITY;
                 pl[k] = pp[ROWS * (D + 1) + i];
+                pu[k] = pp[ROWS * (D + 2) + i];
                 pa[k] = *reinterpret_cast<const f32x4*>(pp + i * D + d);
             }
-            float mn = m;
+            float mn = m, un = unit;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, pm[k]);
+            for (int k = 0; k < 4; ++k) {
+                mn = fmaxf(mn, pm[k]);
+                un = fmaxf(un, pu[k]);
+            }
             const float base = mn == -INFINITY ? 0.0f : mn;
             const float f = __builtin_amdgcn_exp2f(m - base);
             m = mn;
             l *= f;
-            acc *= f;
+            acc *= f * unit_ratio(unit, un);
+            unit = un;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float fk = __builtin_amdgcn_exp2f(pm[k] - base);
                 l = fmaf(pl[k], fk, l);
-                acc += pa[k] * fk;
+                acc += pa[k] * (fk * unit_ratio(pu[k], un));
             }
         }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t tok = row / a.G, head = (int64_t)h * a.G + row - tok * a.G;
     *reinterpret_cast<uint2*>(a.o + (q.row0 + tok) * a.ld_o + head * D + d) =
-        pack_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        pack_bf16(acc[0] * inv * unit, acc[1] * inv * unit, acc[2] * inv * unit, acc[3] * inv * unit);
 }
 
 template <int D, int ROWS>
@@ -132,7 +137,7 @@ Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks)
 size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks) {
     const Form f = form_of(T, R, H / Hk, Hk, D, max_blocks);
     const int64_t grid = f.waves ? 0 : f.rows == kTilesTile ? kTilesShares : kRowsShares;
-    return (size_t)(kv_plan_bytes(R) + 2 * grid * f.rows * (D + 2) * 4);
+    return (size_t)(kv_plan_bytes(R) + 2 * grid * f.rows * (D + 3) * 4);
 }
 
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {

@@ -255,11 +255,19 @@ __device__ __forceinline__ KvPlan kv_plan(const KvAttnArgs& a, const KvRequest& 
 }
 
 // Workspace: int64 [0] units per share, [1 + r] first unit of request r's pairs;
-// then the parts, two per workgroup: sums [ROWS][D], m [ROWS], l [ROWS] (fp32,
-// sums in units of one).
+// then the parts, two per workgroup: sums [ROWS][D], then m, l and vref [ROWS]
+// (fp32).  The sums stay in units of vref until they are divided by l: they hold
+// weights of up to 2^(kLazy + kUp) over all tokens, and times vref would pass fp32's
+// largest where the row itself does not.
 __host__ __device__ inline int64_t kv_plan_bytes(int64_t R) { return ((R + 1) * 8 + 255) / 256 * 256; }
 template <int D, int ROWS>
-constexpr int kv_part_floats = ROWS * (D + 2);
+constexpr int kv_part_floats = ROWS * (D + 3);
+
+// Factor from units of `vref` to units of `most`, the largest of several (0 where
+// no block was seen).
+__device__ __forceinline__ float unit_ratio(float vref, float most) {
+    return most > 0.0f ? vref * __builtin_amdgcn_rcpf(most) : 0.0f;
+}
 
 __device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
 #pragma unroll

@@ -252,15 +252,13 @@ struct RowsState {
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) acc[d] *= vref;
     }
 };
 
-// LDS of W waves: sums [wave][D / 16][64 lanes] float4, then m and l
+// LDS of W waves: sums [wave][D / 16][64 lanes] float4, then m, l and vref
 // [wave][16 rows].
 template <int D, int W>
-constexpr int kXchgFloats = W * kRows * (D + 2);
+constexpr int kXchgFloats = W * kRows * (D + 3);
 
 // Joins the waves' sums; each wave's 16-dim tiles of a row go to o, or to `part`
 // before the division by l.
@@ -271,6 +269,7 @@ __device__ __forceinline__ void join_waves(const KvAttnArgs& a, const KvRequest&
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, col = lane & 15;
     float* xm = xs + W * kRows * D;
     float* xl = xm + W * kRows;
+    float* xu = xl + W * kRows;
     __syncthreads();  // an earlier pair's reads are over
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -278,16 +277,21 @@ __device__ __forceinline__ void join_waves(const KvAttnArgs& a, const KvRequest&
     if (lane < kRows) {
         xm[wv * kRows + col] = st.m;
         xl[wv * kRows + col] = st.l;
+        xu[wv * kRows + col] = st.vref;
     }
     __syncthreads();
-    float f[W], mx = -INFINITY, l = 0.0f;
+    float f[W], mx = -INFINITY, unit = 0.0f, l = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) mx = fmaxf(mx, xm[w * kRows + col]);
+    for (int w = 0; w < W; ++w) {
+        mx = fmaxf(mx, xm[w * kRows + col]);
+        unit = fmaxf(unit, xu[w * kRows + col]);
+    }
     const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         f[w] = __builtin_amdgcn_exp2f(xm[w * kRows + col] - base);
         l = fmaf(xl[w * kRows + col], f[w], l);
+        f[w] *= unit_ratio(xu[w * kRows + col], unit);
     }
     const int64_t i = tile * kRows + col;
     const bool real = i < (int64_t)q.n * a.G;
@@ -306,12 +310,13 @@ __device__ __forceinline__ void join_waves(const KvAttnArgs& a, const KvRequest&
             *reinterpret_cast<f32x4*>(part + col * D + at) = s;
         } else if (real) {
             *reinterpret_cast<uint2*>(a.o + (q.row0 + tok) * a.ld_o + (int64_t)head * D + at) =
-                pack_bf16(s[0] * inv, s[1] * inv, s[2] * inv, s[3] * inv);
+                pack_bf16(s[0] * inv * unit, s[1] * inv * unit, s[2] * inv * unit, s[3] * inv * unit);
         }
     }
     if (part && threadIdx.x < kRows) {
         part[kRows * D + col] = mx;
         part[kRows * (D + 1) + col] = l;
+        part[kRows * (D + 2) + col] = unit;
     }
 }
 

@@ -210,15 +210,15 @@ struct TileState {
     __device__ __forceinline__ void store(const KvAttnArgs& a) const {
         if (!real) return;
         const int hf = (threadIdx.x & 63) >> 5;
-        const float inv = l == 0.0f ? 0.0f : vref / l;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         uint16_t* row = a.o + out + 4 * hf;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<uint2*>(row + d * 32 + 8 * g) =
-                    pack_bf16(acc[d][4 * g] * inv, acc[d][4 * g + 1] * inv, acc[d][4 * g + 2] * inv,
-                              acc[d][4 * g + 3] * inv);
+                    pack_bf16(acc[d][4 * g] * inv * vref, acc[d][4 * g + 1] * inv * vref,
+                              acc[d][4 * g + 2] * inv * vref, acc[d][4 * g + 3] * inv * vref);
     }
     __device__ __forceinline__ void store_part(float* part) const {
         const int lane = threadIdx.x & 63, i = (threadIdx.x >> 6) * 32 + (lane & 31), hf = lane >> 5;
@@ -227,11 +227,11 @@ struct TileState {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4*>(part + i * D + d * 32 + 8 * g + 4 * hf) =
-                    f32x4{acc[d][4 * g] * vref, acc[d][4 * g + 1] * vref, acc[d][4 * g + 2] * vref,
-                          acc[d][4 * g + 3] * vref};
+                    f32x4{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]};
         if (hf == 0) {
             part[kTilesTile * D + i] = m;
             part[kTilesTile * (D + 1) + i] = l;
+            part[kTilesTile * (D + 2) + i] = vref;
         }
     }
 };

@@ -132,3 +132,16 @@ def test_a_rejected_outlier(kt, new):
     c.write([1, 1], [41, 41], torch.bfloat16, big, big)
     c.write([300, 220 + new], [340, 260 + new], torch.bfloat16)
     _check(c, [new] * 2, [340, 260 + new], 2, scale=2.0 ** -40)
+
+
+@pytest.mark.parametrize("kt,D", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_values_near_the_largest(form, kt, D):
+    """Values up to 2^126: the rows are finite, though their sums before the
+    division by the weights' are not."""
+    c, new, lens, H, window = _of_form(form, kt, D)
+    sc = c.ref["scales"].copy()
+    sc[..., 1] *= np.float32(2.0 ** 118)
+    _set(c, sc)
+    _check(c, new, lens, H)
+    _check(c, new, lens, H, window)
