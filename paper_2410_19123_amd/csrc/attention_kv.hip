@@ -130,6 +130,14 @@ Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks)
     return {kTilesTile, tile_pairs >= 384 || blocks <= 16 ? 1 : 0};
 }
 
+// The form of a call.  A request's rows, at most T, lie one after the other, so a
+// window bounds the blocks that any of them sees.
+Form form_of_call(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t max_blocks, int64_t window) {
+    int64_t blocks = max_blocks;
+    if (window > 0 && (window + T) / kKvBlock + 2 < blocks) blocks = (window + T) / kKvBlock + 2;
+    return form_of(T, R, G, Hk, D, blocks);
+}
+
 }  // namespace
 
 // Enough for any window: one that bounds the blocks turns shares into whole pairs,
@@ -141,13 +149,19 @@ size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_
 }
 
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {
-    // A request's rows, at most T, lie one after the other
-    int64_t blocks = a.c.max_blocks;
-    if (a.window > 0 && (a.window + a.c.T) / kKvBlock + 2 < blocks) blocks = (a.window + a.c.T) / kKvBlock + 2;
-    const Form f = form_of(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, blocks);
+    const Form f = form_of_call(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, a.c.max_blocks, a.window);
     const hipError_t e = f.rows == kTilesTile ? launch_attention_tiles(kt, a, f.waves == 0, s)
                                               : launch_attention_rows(kt, a, f.waves, s);
     return e != hipSuccess || f.waves ? e : launch_join(a, f.rows, s);
 }
 
 }  // namespace readme
+
+// Outside readme.h, for tests: the form that readme_attention_kv takes at these
+// sizes, as 256 times the query rows of a pair plus the waves of a workgroup that
+// takes a whole pair (1 for tiles), 0 where shares are dealt.
+extern "C" int32_t readme_internal_attention_kv_form(int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                                     int32_t D, int64_t max_blocks, int64_t window) {
+    const readme::Form f = readme::form_of_call(T, R, H / Hk, Hk, D, max_blocks, window);
+    return f.rows * 256 + f.waves;
+}
