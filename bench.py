@@ -363,14 +363,14 @@ TRAFFIC = {
     # profiles/traffic_gate_up_prefill_skew16.md), or the whole 32-layer stack
     # (profiles/traffic_stack_llama7b_decode32.md)
     "wide_requests": (_GEMM_SOURCES,
-                      "eb360134d14a65267e9ab26150ed9e653bc777b414cce289e968d11007ef77b6",
-                      2369895211, 58720265),
+                      "3836de8cd63628c136c7b4c5c92d154a6e178ef41b61655549ba5c952e0d6ea9",
+                      2369856620, 58720268),
     "prefill_skew16": (_GEMM_SOURCES,
-                       "eb360134d14a65267e9ab26150ed9e653bc777b414cce289e968d11007ef77b6",
-                       610736269, 23068672),
+                       "3836de8cd63628c136c7b4c5c92d154a6e178ef41b61655549ba5c952e0d6ea9",
+                       610475143, 23068672),
     "llama7b_decode32": (_STACK_SOURCES,
-                         "cec68098307e904cd62067ecde548b7f2dadd67ce421becbbd72a61b48e42786",
-                         7875365792, 56098816),
+                         "d024ad651c6d56acf70f943e494083b25d03841c1a0883b4170932bbd62938ae",
+                         7875372326, 56098816),
 }
 
 

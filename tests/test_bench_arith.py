@@ -134,3 +134,10 @@ def test_traffic_sources_hold_the_kernels_that_run():
         Ip = (w.I + 63) // 64 * 64
         tile = fn(0, w.T, 2 * Ip, w.d, w.E, 0, 0, w.layers > 1)
         assert files[tile] in sources and "csrc/gemm.hip" in sources, (name, tile)
+
+
+def test_traffic_entries_are_of_these_sources():
+    """Every entry holds for the sources as they are, so that the lines of bench.py
+    have their traffic."""
+    for name, (_, _, rd, wr) in bench.TRAFFIC.items():
+        assert bench.traffic_bytes(name) == rd + wr, name
