@@ -460,7 +460,9 @@ __device__ __forceinline__ KvBlockRef kv_block_ref(const KvAttnArgs& a, int64_t 
         // of zero are not numbers.
         const bool bad = bad_scales(sc.x, sc.y);
         b.ks = bad ? __builtin_nanf("") : sc.x;
-        b.vs = bad ? __builtin_nanf("") : sc.y;
+        // No scale that the write gives is subnormal; one counts as zero, since its
+        // reciprocal is infinite.
+        b.vs = bad ? __builtin_nanf("") : sc.y < 0x1p-126f ? 0.0f : sc.y;
     }
     return b;
 }

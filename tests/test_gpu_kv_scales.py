@@ -145,3 +145,16 @@ def test_values_near_the_largest(form, kt, D):
     _set(c, sc)
     _check(c, new, lens, H)
     _check(c, new, lens, H, window)
+
+
+@pytest.mark.parametrize("small", [0.0, 1e-40, 2.0 ** -120])
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_under_the_writes(form, small):
+    """Value scales below those that readme_kv_write gives (2^-100), zero and a
+    subnormal among them, beside its smallest."""
+    c, new, lens, H, _ = _of_form(form, "i8", 64)
+    sc = c.ref["scales"].copy()
+    sc[..., 1] = np.float32(2.0 ** -100)
+    sc[c.table[:, 1::3].reshape(-1), :, 1] = np.float32(small)
+    _set(c, sc)
+    _check(c, new, lens, H)
