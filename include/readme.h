@@ -837,9 +837,10 @@ readme_status readme_attention_causal(int64_t T, int32_t H, int32_t R, const int
  *   about 2^-11 of the largest |v| the row sees plus its rounding to bf16,
  *   unless a block that it sees has a value scale above 2^100 times that |v|.
  *   The order of the sums depends on the sizes and lens, never on timing.
- *   A row of q with an infinity or a NaN, one whose largest element is below
- *   2^-100 but not 0, or scores beyond fp32 give an unspecified row; a scale
- *   that is NaN or infinite gives NaN in the rows that see any of its tokens.
+ *   A row of q with an infinity or a NaN, one whose largest element, or that
+ *   times scale, is below 2^-100 but not 0, or scores beyond fp32 give an
+ *   unspecified row; a scale that is NaN or infinite gives NaN in the rows that
+ *   see any of its tokens.
  *   q [T][ld_q] bf16 (head g at columns D g ..), o [T][ld_o] bf16 out, causal
  *   0 or 1, window >= 0, scale > 0 and finite; workspace >=
  *   readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks) bytes,

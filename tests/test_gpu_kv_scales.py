@@ -32,13 +32,13 @@ def _set(c, scales=None, codes=None):
         c.scales.copy_(torch.from_numpy(scales))
 
 
-def _check(c, new, lens, H, window=0, scale=None, causal=True):
+def _check(c, new, lens, H, window=0, scale=None, causal=True, q_scale=1.0):
     """The bound of the header: bf16's half step of the result; of max |v|, fp16's
     half step of every weight, 2^-24 for each weight below its normal numbers, and
     twice the relative error of the weights and their sum (fp32 scores of D
     products, exp2)."""
     off, T, D = _offsets(new), int(sum(new)), c.D
-    q = torch.from_numpy(c.rng.standard_normal((T, H, D))).bfloat16()
+    q = torch.from_numpy(c.rng.standard_normal((T, H, D)) * q_scale).bfloat16()
     scale = D ** -0.5 if scale is None else scale
     o = _lib().readme_attention_kv(KT[c.kt], q.reshape(T, -1).cuda(), _i32(off), _i32(lens), *c.args(),
                                    H=H, scale=scale, causal=causal, window=window)
@@ -158,3 +158,15 @@ def test_scales_under_the_writes(form, small):
     sc[c.table[:, 1::3].reshape(-1), :, 1] = np.float32(small)
     _set(c, sc)
     _check(c, new, lens, H)
+
+
+@pytest.mark.parametrize("qe,scale,ke", [(-38, 2.0 ** -60, 94), (60, 2.0 ** -40, -24), (-95, 1.0, 92)])
+@pytest.mark.parametrize("form", ["rows/8", "tiles/1"])
+def test_scores_of_far_apart_factors(form, qe, scale, ke):
+    """Queries, keys and the softmax scale far from one, their scores of order one:
+    the largest element of a row, and that times scale, from 2^-100 on."""
+    c, new, lens, H, _ = _of_form(form, "i8", 64)
+    sc = c.ref["scales"].copy()
+    sc[..., 0] *= np.float32(2.0 ** ke)
+    _set(c, sc)
+    _check(c, new, lens, H, scale=scale, q_scale=2.0 ** qe)
