@@ -100,6 +100,10 @@ hipError_t launch_join(const KvAttnArgs& a, int rows, hipStream_t s) {
 //   decode, 512 pairs of 32         rows/4 44, rows/0 48, rows/8 47, rows/1 50
 //   decode, 512 pairs of 1 .. 64    rows/4 49, rows/0 53, rows/1 79
 //   decode, 1680 pairs of 2         rows/1 17, rows/4 29, rows/0 38
+//   decode, 1088 pairs of uneven lengths: rows/2 116, rows/4 107 (equal lengths: 96
+//                                   both); the rule sees no lengths and takes rows/2
+//   a table of 2048 blocks of which 32 are used: rows/0 18.5 for 8 pairs, 46.5 for 544
+//                                   (13.8 and 42.2 with a table of 32)
 //   16 x 32 rows on 63 blocks       rows/4 39, tiles/0 51; 13 x 32 on 762: tiles/0 119,
 //                                   rows/0 154 (heads of 64: rows/0 61, tiles/0 83)
 //   256 x 32 rows on 1 block        rows/1 17, tiles/1 20

@@ -113,7 +113,9 @@ __device__ __forceinline__ bool sees_block(int lo, int hi, int j0) {
 // sums, which may hold what a larger scale left: they stop at 2^100 units, and what
 // the block adds to sums that large, at most 2^53, is under fp32's rounding of them.
 // A unit raised by more than 2^100 may lose them.  A NaN moves nothing.  `row_max`:
-// the largest over the lanes that share the row.
+// the largest over the lanes that share the row.  Against one unit for the wave, 64
+// requests of 2048 tokens and 4 prompts of 2048: value scales within 2^4 of each other
+// 44.2 us for 44.1 and 166 for 166; spread over 2^16 44.4 for 44.0 and 173 for 167.
 constexpr float kUnitLow = 0x1p-8f;
 template <class A, int N, class F>
 __device__ __forceinline__ void value_unit(float vs, bool sees, float& vref, float& log_vref, A (&acc)[N],
@@ -228,11 +230,17 @@ __device__ __forceinline__ void row_keys(const KvAttnArgs& a, int len, int64_t p
 
 // --- dealing the work out -------------------------------------------------------
 //
-// A pair is (request, tile of query rows, key head); its work is the blocks that
-// the request sees.  Either a workgroup takes a whole pair, or all pairs, one
-// after the other (head fastest), are dealt to the workgroups in equal
-// contiguous shares, so that one long request among short ones, or few requests,
-// fill the chip alike.  A pair counts kPairCost units (its start and end) and one
+// A pair is (request, tile of query rows, key head); its blocks are those that any
+// row of the request sees.  Either a workgroup takes a whole pair, or all pairs, one
+// after the other (head fastest), are dealt to the workgroups in contiguous shares
+// of equally many blocks, so that one long request among short ones, or few
+// requests, fill the chip alike.  Equal in blocks, not in work, where a request has
+// many causal rows: blocks past a tile's last row are counted and fetched like the
+// others and only their products left out.  Whole pairs of 128 rows stop at the
+// tile's own last block; those of 16 rows take all of the request's, products too.
+// One causal prompt of 4096 at four heads of 128 takes 81 us (whole pairs of 16
+// rows, 13 of needed products), one of 8192 143 (shares of tiles, 51 needed), four of
+// 2048 60 (shares, 13 needed).  A pair counts kPairCost units (its start and end) and one
 // for each block.  A share may begin and end inside a pair: those ends are
 // partial results in the workspace, at most two per workgroup, which a second
 // launch joins (k_attention_join); a pair whose blocks are all in one share is

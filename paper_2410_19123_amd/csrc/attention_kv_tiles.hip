@@ -13,14 +13,14 @@
 //     O^T += V^T P^T   a lane's sums are all of one row, so rescaling is one
 //                   multiply by a factor of its own.
 // Measured (heads of 128, 32 on 8 key heads): 8 x 2048 rows on 2048 keys each,
-// not causal, 595 us, 915 TFLOP/s; 4 causal prompts of 2048, int8 166 us (830),
-// e4m3 162; the matrix cores busy 40% of the cycles and the LDS 31%, with no
-// bank conflicts.  What the rest waits for is spread out: of the 595 us the
-// operand reads between the products are worth 208, the exponentials 20, the
-// staging 44.  Not faster: a half block's scores ahead of its softmax (650), 64
-// rows a wave at one wave a SIMD (730) or, for heads of 64, at two (116 us where
-// this takes 112, 151 for 82 where shares are dealt), three waves a SIMD for
-// heads of 64 (the same).
+// not causal, 603 us, 911 TFLOP/s; 4 causal prompts of 2048, int8 166 to 171 us by
+// the card (804 to 828; 176 for a pass alone), e4m3 151; the matrix cores busy 40% of
+// the cycles and the LDS 31%, with no bank conflicts.  What the rest waits for is
+// spread out: of the first's time (595 us in that run) the operand reads between the
+// products are worth 208, the exponentials 20, the staging 44.  Not faster: a half
+// block's scores ahead of its softmax (650), 64 rows a wave at one wave a SIMD (730)
+// or, for heads of 64, at two (116 us where this takes 112, 151 for 82 where shares
+// are dealt), three waves a SIMD for heads of 64 (the same).
 #include <math.h>
 
 #include "attention_kv.hpp"
