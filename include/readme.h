@@ -27,7 +27,9 @@
  *                             order (routing and grouping done once)
  * Attention over tokens already seen, for the router and a backbone's own
  * layers: readme_kv_write, readme_attention_kv, readme_kv_read (a key/value
- * cache in 8 bits).
+ * cache in 8 bits).  A step with drafted tokens over that cache:
+ * readme_rotary, readme_kv_append, readme_attention_kv_tree,
+ * readme_verify_drafts.
  *
  * Conventions for every call:
  *   - Arrays are DEVICE pointers owned by the caller, row-major, contiguous.
@@ -900,6 +902,159 @@ readme_status readme_router_tf_cached(readme_kv_type kt, int64_t T, int32_t R, i
                                       const void *packed, const void *w_router, const float *bias,
                                       float rms_eps, int32_t *expert_ids, float *logits,
                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rotary positions in general form, beside readme_rope: any even part of a
+ * head, either layout of the pairs, fp32 or bf16, other frequencies.
+ *
+ * readme_rotary_freqs -- host code: freqs[i], i < rot / 2, the angle that one
+ *   position adds to pair i, written to HOST memory (a caller copies it to the
+ *   device once).  f_i = theta^(-2i / rot), then by `scaling`:
+ *     README_ROTARY_PLAIN   f_i
+ *     README_ROTARY_LINEAR  f_i / factor (positions squeezed into the trained
+ *                           range)
+ *     README_ROTARY_BANDED  with n = trained_len f_i / (2 pi), the pair's turns
+ *                           over the trained length, and
+ *                           g = min(1, max(0, (n - low) / (high - low))):
+ *                           f_i (g + (1 - g) / factor), so that fast pairs stay
+ *                           and slow ones are squeezed
+ *   README_ERR_ARG for freqs NULL, theta or factor not positive and finite, and,
+ *   banded, trained_len not positive and finite or not low < high, both finite;
+ *   README_ERR_UNSUPPORTED for rot outside the set below or an unknown scaling.
+ *
+ * readme_rotary -- y = the rows x with the first rot dims of each head turned by
+ *   the row's position, the other dims as they are.  Row t, pair i turns by the
+ *   angle pos[t] * freqs[i] (one fp64 product):
+ *     a' = A (a cos - b sin),  b' = A (b cos + a sin),  A = amplitude
+ *   README_ROTARY_HALF pairs dims i and i + rot / 2, README_ROTARY_PAIRS dims
+ *   2i and 2i + 1.  inverse = 1 turns back (sin negated): with the same A that is
+ *   the gradient, x_grad = readme_rotary(y_grad), of the call with inverse = 0.
+ *   The angle is reduced in fp64, sine, cosine and products are fp32, so that
+ *   a' and b' are the exact results up to 2^-21 A (|a| + |b|) and, in bf16, one
+ *   rounding.  Angles beyond 2^50 and frequencies that are not finite give
+ *   unspecified values.
+ *     x [T][ld_x], y [T][ld_y] dt, H heads of D dims at columns D h ..;
+ *     pos [T] int32, of any sign; freqs [rot / 2] fp64 (device)
+ *   y may be x itself (with ld_y = ld_x); apart from that they must not overlap.
+ *   Requires D a multiple of 16 and at most 512, rot a multiple of 16 and
+ *   16 <= rot <= D, H <= 65535, T (D / 16) <= 2^31, row strides at least H D and
+ *   multiples of 16 bytes, x and y 16-byte aligned, freqs 8-byte aligned,
+ *   amplitude finite.
+ */
+typedef int32_t readme_rotary_layout;
+#define README_ROTARY_HALF 0
+#define README_ROTARY_PAIRS 1
+#define README_ROTARY_PLAIN 0
+#define README_ROTARY_LINEAR 1
+#define README_ROTARY_BANDED 2
+readme_status readme_rotary_freqs(int32_t rot, double theta, int32_t scaling, double factor,
+                                  double trained_len, double low, double high, double *freqs);
+readme_status readme_rotary(readme_dtype dt, int64_t T, int32_t H, int32_t D, int32_t rot,
+                            readme_rotary_layout layout, int32_t inverse, float amplitude,
+                            const int32_t *pos, const double *freqs, const void *x, int64_t ld_x,
+                            void *y, int64_t ld_y, void *stream);
+
+/*
+ * readme_kv_append -- readme_kv_write with the keys turned by their positions on
+ * the way: the cache ends up, bit for bit, as after readme_rotary (inverse 0) of
+ * the keys in fp32 (k converted to fp32 if it is bf16) and readme_kv_write of the
+ * turned fp32 keys and of v.  The turned keys are never rounded to bf16.
+ *   pos [T] int32 the rows' positions for the rotation (a draft's is its depth in
+ *   the tree past the last certain token, not its slot), or NULL: the position
+ *   lens[r] - n_r + i that the row is stored at.  rot, layout, amplitude and freqs
+ *   as in readme_rotary, everything else as in readme_kv_write.
+ */
+readme_status readme_kv_append(readme_kv_type kt, readme_dtype dt, int64_t T, int32_t R, int32_t Hk,
+                               int32_t D, int32_t rot, readme_rotary_layout layout,
+                               float amplitude, const int32_t *pos, const double *freqs,
+                               const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                               const int32_t *offsets, const int32_t *lens, const int32_t *table,
+                               int64_t max_blocks, int64_t n_blocks, void *codes, float *scales,
+                               void *stream);
+
+/*
+ * readme_attention_kv_tree -- readme_attention_kv for rows that do not follow
+ * one another, such as a tree of drafted tokens: of its request's last n_r
+ * tokens in the cache, which are the call's own rows, a row sees those that its
+ * bits name, and of the tokens before them all.
+ *   tree [T][words] uint64  bit b % 64 of tree[i][b / 64] set: row i sees the
+ *                    b-th row of its request (its own bit among them), at
+ *                    position first + b, first = lens[r] - n_r; bits from n_r on
+ *                    mean nothing, rows from 64 words on are seen by none
+ *   pos  [T] int32   or NULL: the rows' positions where window > 0: of the tokens
+ *                    before `first` row i sees those at
+ *                    j > max(pos[i], first) - window.  NULL: first + the row's
+ *                    place in the request.  The call's own rows are not cut off
+ *                    by the window.
+ * Never absent tokens; a row that sees no token is zeros.  Everything else, the
+ * precision among it, is as in readme_attention_kv; workspace >=
+ * readme_attention_kv_tree_workspace_bytes(T, R, H, Hk, D, max_blocks).  Requires
+ * 1 <= words <= 65536 and tree 8-byte aligned.
+ */
+size_t readme_attention_kv_tree_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                                int32_t D, int64_t max_blocks);
+readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, int32_t H,
+                                       int32_t Hk, int32_t D, const void *q, int64_t ld_q,
+                                       const int32_t *offsets, const int32_t *lens,
+                                       const int32_t *table, int64_t max_blocks, int64_t n_blocks,
+                                       const void *codes, const float *scales,
+                                       const uint64_t *tree, int32_t words, const int32_t *pos,
+                                       float scale, int64_t window, void *o, int64_t ld_o,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * readme_verify_drafts -- which drafted tokens a target model takes, and the
+ * token after them, so that what comes out is distributed as if the target had
+ * drawn every token itself (rejection sampling with the residual distribution).
+ *
+ * Request r's rows i = 0 .. n_r - 1 of the call ([offsets[r], offsets[r+1]), as in
+ * the cache's calls) are a tree: row 0 the last certain token, row i > 0 the draft
+ * tokens[i] below row parent[i] < i (a place in the request; a draft whose parent
+ * lies outside [0, i) is below none).  A row's p is the target's distribution of
+ * the token after it, its q the one that the drafts below it were drawn from.
+ *   From node = row 0, with t = p of the node and a = 1, the drafts below the node
+ *   are tried in ascending row order.  Draft i, of token x, is taken if
+ *     u[i] * a * q(x) < t(x)
+ *   and is then the node, t its p and a = 1.  Otherwise it is refused:
+ *     t(v) = max(t(v) - a q(v), 0),  W = sum_v t(v),  a = W / S,
+ *   S = 1; or, if distinct = 1 (the drafts of a node were drawn without
+ *   replacement), S = the sum of q(v) over the v that were not refused at the node,
+ *   and q(x) = 0 from here on (a = 0 if S = 0).  If W = 0, t and a stay as they were
+ *   and the node's other drafts are passed over.
+ *   When no draft is left, the next token is the least v with
+ *     t(0) + .. + t(v) > u[row 0] * sum_v t(v).
+ * All of it in fp64; p and q as given, neither need sum to 1 exactly; entries that
+ * are negative or NaN count as 0, and so do p and q of a token outside [0, V).
+ *   dt, p [T][ld_p], q [T][ld_q]  bf16 or fp32; q NULL: the drafts were certain
+ *                    (q(v) = 1 at the draft's own token, 0 elsewhere)
+ *   tokens, parent [T] int32 (row 0's are not read); u [T] fp32 random numbers in
+ *                    [0, 1)
+ *   path     [T] int32 out  path[offsets[r] + j]: the place in the request of the
+ *                    j-th node, row 0 first; -1 after the last.  Rows from
+ *                    offsets[R] on are not written.
+ *   accepted [R] int32 out  drafts taken
+ *   token    [R] int32 out  the token after them; -1 where there is none (no rows,
+ *                    or t = 0 everywhere)
+ *   workspace >= readme_verify_drafts_workspace_bytes(T, R, V) bytes (it may be 0
+ *                    bytes, then workspace may be NULL), 16-byte aligned, contents
+ *                    unspecified before and after; calls in flight together need
+ *                    workspaces of their own.
+ * p and q are read for the nodes on the path alone.  Rows of a request from
+ * README_MAX_DRAFT_ROWS on are not tried.  The taken rows' keys and values lie in
+ * the cache behind each other only if the tree was a chain; else they are read
+ * (readme_kv_read), and written where they belong with the new lens.
+ * T = 0 still writes accepted and token.  Requires 1 <= V < 2^31, T <= 2^27,
+ * R <= 2^20, R V <= 2^36, row strides at least V and multiples of 16 bytes, p and q
+ * 16-byte aligned, the other arrays 4-byte aligned.
+ */
+#define README_MAX_DRAFT_ROWS 1024
+size_t readme_verify_drafts_workspace_bytes(int64_t T, int32_t R, int64_t V);
+readme_status readme_verify_drafts(readme_dtype dt, int64_t T, int32_t R, int64_t V,
+                                   const int32_t *offsets, const int32_t *tokens,
+                                   const int32_t *parent, const void *p, int64_t ld_p,
+                                   const void *q, int64_t ld_q, const float *u, int32_t distinct,
+                                   int32_t *path, int32_t *accepted, int32_t *token,
+                                   void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,9 @@ LIB_PATH = os.path.join(_PKG, "libreadme.so")
 README_F32, README_BF16 = 0, 1
 README_KV_I8, README_KV_E4M3 = 0, 1
 README_KV_BLOCK = 64
+README_ROTARY_HALF, README_ROTARY_PAIRS = 0, 1
+README_ROTARY_PLAIN, README_ROTARY_LINEAR, README_ROTARY_BANDED = 0, 1, 2
+README_MAX_DRAFT_ROWS = 1024
 README_MAX_EXPERTS = 256
 README_MAX_PERMANENT_SLICES = 16
 
@@ -28,6 +31,7 @@ _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported size or type",
 # (name, restype, argtypes) of every exported symbol of readme.h.
 _P, _I64, _I32, _SZ, _F = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
                            ctypes.c_size_t, ctypes.c_float)
+_D = ctypes.c_double
 SIGNATURES = {
     "readme_status_string": (ctypes.c_char_p, [_I32]),
     "readme_abi_version": (_I32, []),
@@ -106,6 +110,18 @@ SIGNATURES = {
     "readme_attention_kv_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I64]),
     "readme_attention_kv": (_I32, [_I32, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P, _I64,
                                    _I64, _P, _P, _F, _I32, _I64, _P, _I64, _P, _SZ, _P]),
+    "readme_rotary_freqs": (_I32, [_I32, _D, _I32, _D, _D, _D, _D, _P]),
+    "readme_rotary": (_I32, [_I32, _I64, _I32, _I32, _I32, _I32, _I32, _F, _P, _P, _P, _I64, _P,
+                             _I64, _P]),
+    "readme_kv_append": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I32, _F, _P, _P, _P,
+                                _I64, _P, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P]),
+    "readme_attention_kv_tree_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I64]),
+    "readme_attention_kv_tree": (_I32, [_I32, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P,
+                                        _I64, _I64, _P, _P, _P, _I32, _P, _F, _I64, _P, _I64, _P,
+                                        _SZ, _P]),
+    "readme_verify_drafts_workspace_bytes": (_SZ, [_I64, _I32, _I64]),
+    "readme_verify_drafts": (_I32, [_I32, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _P, _I64, _P,
+                                    _I32, _P, _P, _P, _P, _SZ, _P]),
 }
 
 # Workspace regions of readme_router_tf (README_RTF_*).
@@ -945,6 +961,161 @@ def readme_router_tf_cached(kt: int, tokens, req_offsets, lens, table, codes, sc
              _p(bias), rms_eps, _p(expert_ids), _p(logits), _p(workspace),
              workspace.numel() * workspace.element_size())
     return expert_ids, logits, workspace
+
+
+# --- a step with drafted tokens over the cache --------------------------------
+
+def readme_rotary_freqs(rot: int, theta: float = 10000.0, scaling: int = README_ROTARY_PLAIN,
+                        factor: float = 1.0, trained_len: float = 0.0, low: float = 1.0,
+                        high: float = 32.0, device=None):
+    """The angle one position adds to each pair: fp64 [rot / 2], computed on the
+    host, on `device` if one is given."""
+    f = torch.empty(max(rot // 2, 0), dtype=torch.float64)
+    _call("readme_rotary_freqs", rot, theta, scaling, factor, trained_len, low, high, _p(f))
+    return f if device is None else f.to(device)
+
+
+def _freqs_args(freqs, dev: int) -> int:
+    """rot of the frequencies."""
+    if freqs.dtype is not torch.float64 or freqs.dim() != 1:
+        raise ValueError("freqs must be fp64 [rot / 2]")
+    _on(dev, freqs=freqs)
+    return 2 * freqs.shape[0]
+
+
+def _on(dev: int, **tensors) -> None:
+    """Tensors (or None) must be contiguous, on device `dev`."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.get_device() != dev:
+            raise ValueError(f"{name} must be on the call's device")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _vector(t, n: int, dtype, name: str) -> None:
+    if t is not None and (t.dtype is not dtype or t.shape != (n,)):
+        raise ValueError(f"{name} must be {dtype} [{n}]")
+
+
+def readme_rotary(x, pos, freqs, D: int, layout: int = README_ROTARY_HALF, amplitude: float = 1.0,
+                  inverse: bool = False, y=None):
+    """Rows x ([T][H D], bf16 or fp32; slices of wider rows allowed) with the first
+    2 len(freqs) dims of each head of D turned by pos; returns y, which may be x.
+    inverse turns back: the gradient of the call without it."""
+    dev = x.get_device()
+    if dev < 0:
+        raise ValueError("libreadme takes device tensors")
+    if x.dim() != 2 or D < 1 or x.shape[1] % D:
+        raise ValueError("x must be [T][H D]")
+    T, width = x.shape
+    if y is None:
+        y = torch.empty((T, width), dtype=x.dtype, device=x.device)
+    if y.dtype is not x.dtype:
+        raise ValueError("x and y dtypes disagree")
+    ld_x, ld_y = _kv_rows(x, T, width, dev, "x"), _kv_rows(y, T, width, dev, "y")
+    rot = _freqs_args(freqs, dev)
+    _vector(pos, T, torch.int32, "pos")
+    _on(dev, pos=pos)
+    _kv_call(dev, "readme_rotary", _dt(x), T, width // D, D, rot, layout, 1 if inverse else 0,
+             amplitude, pos.data_ptr(), freqs.data_ptr(), x.data_ptr(), ld_x, y.data_ptr(), ld_y)
+    return y
+
+
+def readme_kv_append(kt: int, k, v, offsets, lens, table, codes, scales, freqs, pos=None,
+                     layout: int = README_ROTARY_HALF, amplitude: float = 1.0) -> None:
+    """readme_kv_write with the keys turned by their positions (pos [T], or None:
+    those they are stored at) on the way."""
+    R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
+    T = k.shape[0]
+    ld_k, ld_v = _kv_rows(k, T, Hk * D, dev, "k"), _kv_rows(v, T, Hk * D, dev, "v")
+    if v.dtype is not k.dtype:
+        raise ValueError("k and v dtypes disagree")
+    rot = _freqs_args(freqs, dev)
+    _vector(pos, T, torch.int32, "pos")
+    _on(dev, pos=pos)
+    _kv_call(dev, "readme_kv_append", kt, _dt(k), T, R, Hk, D, rot, layout, amplitude,
+             None if pos is None else pos.data_ptr(), freqs.data_ptr(), k.data_ptr(), ld_k,
+             v.data_ptr(), ld_v, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb,
+             codes.data_ptr(), scales.data_ptr())
+
+
+def readme_attention_kv_tree_workspace_bytes(T: int, R: int, H: int, Hk: int, D: int,
+                                             max_blocks: int) -> int:
+    return int(load().readme_attention_kv_tree_workspace_bytes(T, R, H, Hk, D, max_blocks))
+
+
+def readme_attention_kv_tree(kt: int, q, offsets, lens, table, codes, scales, H: int, tree,
+                             pos=None, scale=None, window: int = 0, o=None, workspace=None):
+    """Attention of query rows q over the cache, each seeing the tokens before the
+    call's and those of the call's own rows that its bits in tree (int64
+    [T][words]) name; scale defaults to 1 / sqrt(D).  Returns o [T][H D]."""
+    R, Hk, D, mb, nb, dev = _kv_cache_args(offsets, lens, table, codes, scales)
+    T = q.shape[0]
+    if o is None:
+        o = torch.empty((T, H * D), dtype=torch.bfloat16, device=codes.device)
+    if q.dtype is not torch.bfloat16 or o.dtype is not torch.bfloat16:
+        raise ValueError("q and o must be bf16")
+    ld_q, ld_o = _kv_rows(q, T, H * D, dev, "q"), _kv_rows(o, T, H * D, dev, "o")
+    if tree.dtype is not torch.int64 or tree.dim() != 2 or tree.shape[0] != T:
+        raise ValueError("tree must be int64 [T][words]")
+    _vector(pos, T, torch.int32, "pos")
+    _on(dev, tree=tree, pos=pos, workspace=workspace)
+    if workspace is None:
+        ws = readme_attention_kv_tree_workspace_bytes(T, R, H, Hk, D, mb)
+        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=codes.device)
+    _kv_call(dev, "readme_attention_kv_tree", kt, T, R, H, Hk, D, q.data_ptr(), ld_q,
+             offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb, codes.data_ptr(),
+             scales.data_ptr(), tree.data_ptr(), tree.shape[1],
+             None if pos is None else pos.data_ptr(), D ** -0.5 if scale is None else scale, window,
+             o.data_ptr(), ld_o, workspace.data_ptr(), workspace.nbytes)
+    return o
+
+
+def readme_verify_drafts_workspace_bytes(T: int, R: int, V: int) -> int:
+    return int(load().readme_verify_drafts_workspace_bytes(T, R, V))
+
+
+def readme_verify_drafts(offsets, tokens, parent, p, q, u, distinct: bool = False, path=None,
+                         accepted=None, token=None, workspace=None):
+    """Which drafted tokens the target distributions p ([T][V], bf16 or fp32; slices
+    of wider rows allowed) take, given the drafts' own q (None: certain drafts) and
+    the random numbers u [T]; returns (path [T], accepted [R], token [R])."""
+    dev = p.get_device()
+    if dev < 0:
+        raise ValueError("libreadme takes device tensors")
+    if p.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("p must be [T][V] and offsets [R+1]")
+    T, V = p.shape
+    R = offsets.shape[0] - 1
+    i32 = torch.int32
+    new = {"dtype": i32, "device": p.device}
+    path = torch.empty(T, **new) if path is None else path
+    accepted = torch.empty(R, **new) if accepted is None else accepted
+    token = torch.empty(R, **new) if token is None else token
+    for t, n, name in ((offsets, R + 1, "offsets"), (tokens, T, "tokens"), (parent, T, "parent"),
+                       (path, T, "path"), (accepted, R, "accepted"), (token, R, "token")):
+        _vector(t, n, i32, name)
+    _vector(u, T, torch.float32, "u")
+    one = 16 // p.element_size()
+    row = -(-V // one) * one  # the stride of a single row, which has none
+    ld_p, ld_q = _kv_rows(p, T, V, dev, "p") if T > 1 else row, 0
+    if q is not None:
+        if q.dtype is not p.dtype:
+            raise ValueError("p and q dtypes disagree")
+        ld_q = _kv_rows(q, T, V, dev, "q")
+        ld_q = ld_q if T > 1 else row
+    if workspace is None:
+        ws = readme_verify_drafts_workspace_bytes(T, R, V)
+        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=p.device)
+    _on(dev, offsets=offsets, tokens=tokens, parent=parent, u=u, path=path, accepted=accepted,
+        token=token, workspace=workspace)
+    _kv_call(dev, "readme_verify_drafts", _dt(p), T, R, V, offsets.data_ptr(), tokens.data_ptr(),
+             parent.data_ptr(), p.data_ptr(), ld_p, None if q is None else q.data_ptr(), ld_q,
+             u.data_ptr(), 1 if distinct else 0, path.data_ptr(), accepted.data_ptr(),
+             token.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+    return path, accepted, token
 
 
 def readme_status_string(status: int) -> str:

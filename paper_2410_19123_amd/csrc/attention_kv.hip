@@ -154,8 +154,13 @@ size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_
 
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {
     const Form f = form_of_call(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, a.c.max_blocks, a.window);
-    const hipError_t e = f.rows == kTilesTile ? launch_attention_tiles(kt, a, f.waves == 0, s)
-                                              : launch_attention_rows(kt, a, f.waves, s);
+    hipError_t e;
+    if (a.tree)
+        e = f.rows == kTilesTile ? launch_attention_tree_tiles(kt, a, f.waves == 0, s)
+                                 : launch_attention_tree_rows(kt, a, f.waves, s);
+    else
+        e = f.rows == kTilesTile ? launch_attention_tiles(kt, a, f.waves == 0, s)
+                                 : launch_attention_rows(kt, a, f.waves, s);
     return e != hipSuccess || f.waves ? e : launch_join(a, f.rows, s);
 }
 

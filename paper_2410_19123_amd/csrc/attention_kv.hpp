@@ -1,5 +1,7 @@
 // Shared by the two attention kernels over the 8-bit cache
-// (attention_kv_rows.hip: few query rows, attention_kv_tiles.hip: many).
+// (attention_kv_rows.hpp: few query rows, attention_kv_tiles.hpp: many), each with
+// rows that follow one another and with rows of a draft tree (TREE), which differ
+// in the keys that a row sees alone.
 //
 // For a query row i (a token and one of the G query heads of a key head) at
 // position p and the keys j it sees (j < len; j <= p if causal; j > p - window)
@@ -157,13 +159,60 @@ __device__ __forceinline__ float score_offset(float log_r, float m) {
     return log_r + kUp - (m == -INFINITY ? 0.0f : m);
 }
 
+// Rows of a draft tree: row t of the request sees the tokens [lo, first) and of the
+// request's own rows, at first .. len - 1, those of its bits.  Blocks that all rows
+// see whole, between their largest lo and first, ask for no bits; word 0 of them is
+// loaded with the row.
+struct TreeRow {
+    const uint64_t* bits;
+    uint64_t word0;
+    int lo, first;
+
+    // t < 0: there is no row, and no token is seen.
+    __device__ __forceinline__ void set(const KvAttnArgs& a, int64_t row0, int n, int len, int64_t t) {
+        const int64_t f = (int64_t)len - n;
+        first = (int)f;
+        lo = first < 0 ? 0 : first;
+        bits = a.tree + (row0 + (t < 0 ? 0 : t)) * a.words;
+        word0 = 0;
+        if (t < 0) return;
+        word0 = bits[0];
+        int64_t l = 0;
+        if (a.window > 0) {
+            const int64_t p = a.pos ? (int64_t)a.pos[row0 + t] : f + t;
+            l = (p < f ? f : p) - a.window + 1;
+        }
+        lo = (int)(l < 0 ? 0 : (l < lo ? l : lo));
+    }
+    __device__ __forceinline__ uint64_t word(const KvAttnArgs& a, int i) const {
+        return i == 0 ? word0 : (i < a.words ? bits[i] : 0);
+    }
+    // Bit s: the row sees token j0 + s.
+    __device__ __forceinline__ uint64_t seen(const KvAttnArgs& a, int j0, int len) const {
+        const int l = lo - j0, f = first - j0, e = len - j0;
+        uint64_t m = ones_below(f) & ~ones_below(l);
+        if (f < kKvBlock) {
+            uint64_t own;
+            if (f > 0) {
+                own = word0 << f;
+            } else {
+                const int w = -f >> 6, sh = -f & 63;
+                own = word(a, w) >> sh;
+                if (sh) own |= word(a, w + 1) << (64 - sh);
+            }
+            m |= own & ones_below(e);
+        }
+        return m;
+    }
+    __device__ __forceinline__ static uint64_t ones_below(int n) {
+        return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1);
+    }
+};
+
 // A block whose key or value scale is not finite: every row that sees any of its
 // tokens becomes NaN through its sum (the factor and offset above stay finite, so
 // other rows' weights for it are 0).
 __device__ __forceinline__ bool bad_scales(float ks, float vs) { return !(ks < INFINITY && vs < INFINITY); }
-__device__ __forceinline__ float bad_sum(float l, int lo, int hi, int j0) {
-    return sees_block(lo, hi, j0) ? __builtin_nanf("") : l;
-}
 
 // Token k of a lane's 16 is seen if a0 <= k < a1.
 template <class V>
@@ -171,6 +220,13 @@ __device__ __forceinline__ void mask_scores(V& v, int a0, int a1) {
 #pragma unroll
     for (int k = 0; k < 16; ++k)
         v[k] = (unsigned)(k - a0) < (unsigned)(a1 - a0) ? v[k] : -INFINITY;
+}
+
+// Token k of a lane's 16 is seen if bit k is set.
+template <class V>
+__device__ __forceinline__ void mask_bits(V& v, uint32_t bits) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = (bits >> k) & 1u ? v[k] : -INFINITY;
 }
 
 // Query rows as fp16 matrix operands.  Each lane holds elements of one row in
@@ -489,5 +545,8 @@ constexpr int kTilesShares = 512;
 // `waves` of a workgroup that takes a whole pair (1, 2, 4, 8), or 0 for shares.
 hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attention_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
+// The same with a.tree.
+hipError_t launch_attention_tree_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_attention_tree_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
 
 }  // namespace readme

@@ -1,0 +1,10 @@
+// The kernels of attention_kv_tiles.hpp for rows of a draft tree.
+#include "attention_kv_tiles.hpp"
+
+namespace readme {
+
+hipError_t launch_attention_tree_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s) {
+    return tiles_by_type<true>(kt, a, shares, s);
+}
+
+}  // namespace readme

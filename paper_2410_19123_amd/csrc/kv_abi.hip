@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include "kv_cache.hpp"
+#include "rotary.hpp"
 
 using namespace readme;
 
@@ -21,6 +22,9 @@ constexpr int64_t kMaxWindow = 1ll << 33;
 inline readme_status st_of(hipError_t e) { return e == hipSuccess ? README_OK : README_ERR_HIP; }
 inline bool al(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+
+constexpr float kLog2e = 1.4426950408889634f;  // weights are powers of two
+constexpr int32_t kMaxWords = 65536;           // of a row's bits in a draft tree
 
 bool head_dim_ok(int32_t D) { return D == 64 || D == 128 || D == 256; }
 
@@ -87,6 +91,38 @@ KvCacheArgs kv_cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int
 
 }  // namespace readme
 
+namespace {
+
+// Checks of both attention calls, and what their kernels take alike.
+readme_status attention_args(readme_kv_type kt, int64_t T, int32_t R, int32_t H, int32_t Hk,
+                             int32_t D, const void* q, int64_t ld_q, const int32_t* offsets,
+                             const int32_t* lens, const int32_t* table, int64_t max_blocks,
+                             int64_t n_blocks, const void* codes, const float* scales, float score,
+                             int64_t window, void* o, int64_t ld_o, void* workspace,
+                             size_t workspace_bytes, KvAttnArgs* a, bool* done) {
+    readme_status st = kv_check_attention(kt, T, R, H, Hk, D, max_blocks, n_blocks, done);
+    if (st != README_OK || *done) return st;
+    a->c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes, scales);
+    if ((st = kv_check_cache(a->c)) != README_OK) return st;
+    const int64_t width = (int64_t)H * D;
+    if ((st = check_rows(q, ld_q, width, 2)) != README_OK) return st;
+    if ((st = check_rows(o, ld_o, width, 2)) != README_OK) return st;
+    if (!workspace || !al(workspace, 16)) return README_ERR_ARG;
+    if (workspace_bytes < kv_attention_workspace(T, R, H, Hk, D, max_blocks))
+        return README_ERR_WORKSPACE;
+    a->q = reinterpret_cast<const uint16_t*>(q);
+    a->ld_q = ld_q;
+    a->o = reinterpret_cast<uint16_t*>(o);
+    a->ld_o = ld_o;
+    a->G = H / Hk;
+    a->score = score;
+    a->window = window < kMaxWindow ? window : kMaxWindow;
+    a->ws = workspace;
+    return README_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 size_t readme_kv_codes_bytes(int64_t n_blocks, int32_t Hk, int32_t D) {
@@ -115,6 +151,35 @@ readme_status readme_kv_write(readme_kv_type kt, readme_dtype dt, int64_t T, int
     if ((st = check_rows(k, ld_k, width, es)) != README_OK) return st;
     if ((st = check_rows(v, ld_v, width, es)) != README_OK) return st;
     return st_of(launch_kv_write(kt, dt, c, k, ld_k, v, ld_v, as_stream(stream)));
+}
+
+readme_status readme_kv_append(readme_kv_type kt, readme_dtype dt, int64_t T, int32_t R, int32_t Hk,
+                               int32_t D, int32_t rot, readme_rotary_layout layout,
+                               float amplitude, const int32_t* pos, const double* freqs,
+                               const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                               const int32_t* offsets, const int32_t* lens, const int32_t* table,
+                               int64_t max_blocks, int64_t n_blocks, void* codes, float* scales,
+                               void* stream) {
+    if (dt != README_F32 && dt != README_BF16) return README_ERR_UNSUPPORTED;
+    bool done;
+    readme_status st = check_sizes(kt, T, R, Hk, Hk, D, max_blocks, n_blocks, &done);
+    if (st != README_OK) return st;
+    if ((st = rotary_check_sizes(D, rot, layout, 0, amplitude)) != README_OK || done) return st;
+    const KvCacheArgs c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
+                                     scales);
+    if ((st = kv_check_cache(c)) != README_OK) return st;
+    if (!freqs || !al(freqs, 8) || !al(pos, 4)) return README_ERR_ARG;
+    const int64_t es = (int64_t)dtype_size(dt), width = (int64_t)Hk * D;
+    if ((st = check_rows(k, ld_k, width, es)) != README_OK) return st;
+    if ((st = check_rows(v, ld_v, width, es)) != README_OK) return st;
+    RotaryArgs a;
+    a.pos = pos;
+    a.freqs = freqs;
+    a.amplitude = amplitude;
+    a.rot = rot;
+    a.layout = layout;
+    a.inverse = 0;
+    return st_of(launch_kv_append(kt, dt, c, a, k, ld_k, v, ld_v, as_stream(stream)));
 }
 
 readme_status readme_kv_read(readme_kv_type kt, readme_dtype dt, int64_t T, int32_t R, int32_t Hk,
@@ -150,32 +215,46 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
                                   float scale, int32_t causal, int64_t window, void* o,
                                   int64_t ld_o, void* workspace, size_t workspace_bytes,
                                   void* stream) {
-    const float score = scale * 1.4426950408889634f;  // log2(e): weights are powers of two
+    const float score = scale * kLog2e;
     if (causal < 0 || causal > 1 || window < 0 || !(score > 0.0f) || !isfinite(score))
         return README_ERR_ARG;
-    bool done;
-    readme_status st = kv_check_attention(kt, T, R, H, Hk, D, max_blocks, n_blocks, &done);
-    if (st != README_OK || done) return st;
-    const KvCacheArgs c = kv_cache_args(T, R, Hk, D, offsets, lens, table, max_blocks, n_blocks, codes,
-                                     scales);
-    if ((st = kv_check_cache(c)) != README_OK) return st;
-    const int64_t width = (int64_t)H * D;
-    if ((st = check_rows(q, ld_q, width, 2)) != README_OK) return st;
-    if ((st = check_rows(o, ld_o, width, 2)) != README_OK) return st;
-    if (!workspace || !al(workspace, 16)) return README_ERR_ARG;
-    if (workspace_bytes < kv_attention_workspace(T, R, H, Hk, D, max_blocks))
-        return README_ERR_WORKSPACE;
     KvAttnArgs a{};
-    a.c = c;
-    a.q = reinterpret_cast<const uint16_t*>(q);
-    a.ld_q = ld_q;
-    a.o = reinterpret_cast<uint16_t*>(o);
-    a.ld_o = ld_o;
-    a.G = H / Hk;
-    a.score = score;
+    bool done;
+    const readme_status st =
+        attention_args(kt, T, R, H, Hk, D, q, ld_q, offsets, lens, table, max_blocks, n_blocks, codes,
+                       scales, score, window, o, ld_o, workspace, workspace_bytes, &a, &done);
+    if (st != README_OK || done) return st;
     a.causal = causal;
-    a.window = window < kMaxWindow ? window : kMaxWindow;
-    a.ws = workspace;
+    return st_of(launch_kv_attention(kt, a, as_stream(stream)));
+}
+
+size_t readme_attention_kv_tree_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                                int32_t D, int64_t max_blocks) {
+    return readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks);
+}
+
+readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, int32_t H,
+                                       int32_t Hk, int32_t D, const void* q, int64_t ld_q,
+                                       const int32_t* offsets, const int32_t* lens,
+                                       const int32_t* table, int64_t max_blocks, int64_t n_blocks,
+                                       const void* codes, const float* scales,
+                                       const uint64_t* tree, int32_t words, const int32_t* pos,
+                                       float scale, int64_t window, void* o, int64_t ld_o,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+    const float score = scale * kLog2e;
+    if (window < 0 || !(score > 0.0f) || !isfinite(score)) return README_ERR_ARG;
+    if (words < 1) return README_ERR_ARG;
+    if (words > kMaxWords) return README_ERR_UNSUPPORTED;
+    KvAttnArgs a{};
+    bool done;
+    const readme_status st =
+        attention_args(kt, T, R, H, Hk, D, q, ld_q, offsets, lens, table, max_blocks, n_blocks, codes,
+                       scales, score, window, o, ld_o, workspace, workspace_bytes, &a, &done);
+    if (st != README_OK || done) return st;
+    if (!tree || !al(tree, 8) || !al(pos, 4)) return README_ERR_ARG;
+    a.tree = tree;
+    a.words = words;
+    a.pos = pos;
     return st_of(launch_kv_attention(kt, a, as_stream(stream)));
 }
 

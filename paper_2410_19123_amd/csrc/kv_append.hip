@@ -1,0 +1,83 @@
+// readme_kv_append: a call's keys, turned by their positions, and values into the
+// 8-bit cache (rotary.hpp and kv_cache.hip have the mathematics).
+//
+// The write's own kernel with another source of K rows: a thread's sixteen dims
+// are the two runs of eight whose pairs they make, so both members of a pair and
+// its angle are in one thread and the turned fp32 values go from its registers into
+// the codes.
+#include "kv_write.hpp"
+
+namespace readme {
+
+namespace {
+
+// The call's key rows, turned.
+template <int DT>
+struct TurnedRows {
+    static constexpr int kType = README_F32;
+    static constexpr bool kOneRun = false;
+    static constexpr int N = DT == README_F32 ? 2 : 1;
+    struct Raw {
+        uint4 a[N], b[N];
+    };
+    const void* base;
+    int64_t ld;
+    RotaryArgs rot;
+
+    __device__ __forceinline__ Chunk chunk(int ch) const { return chunk_of(ch, rot.rot, rot.layout); }
+    __device__ __forceinline__ void zero(Raw& x) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x.a[i] = x.b[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void load(Raw& x, int64_t tok, int col, int ch) const {
+        const Chunk k = chunk(ch);
+        load8<DT>(base, tok * ld + col + k.a, x.a);
+        load8<DT>(base, tok * ld + col + k.b, x.b);
+    }
+    // Row `row` of the block's rows; zeros past the last.
+    __device__ __forceinline__ Row16<README_F32> value(const Raw& x, const Touched& b, int row, int ch) const {
+        float v[16];
+        widen8<DT>(x.a, v);
+        widen8<DT>(x.b, v + 8);
+        if (chunk(ch).turns && row < b.n) {
+            const double pos = rot.pos ? (double)rot.pos[b.tok + row]
+                                       : (double)(b.j * kKvBlock + b.slot + row);
+            Turn t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = turn_of(pos, rot.freqs[8 * ch + e], rot.amplitude, 1.0f);
+            turn_chunk(t, rot.layout, v);
+        }
+        Row16<README_F32> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o.v[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+        return o;
+    }
+};
+
+template <int KT, int DT, int D>
+__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvCacheArgs c, RotaryArgs rot,
+                                                          const void* __restrict__ k, int64_t ld_k,
+                                                          const void* __restrict__ v, int64_t ld_v) {
+    write_candidate<KT, D>(c, TurnedRows<DT>{k, ld_k, rot}, PlainRows<DT>{v, ld_v});
+}
+
+template <int KT, int DT, int D>
+struct AppendOp {
+    static hipError_t go(KvCacheArgs c, RotaryArgs rot, const void* k, int64_t ld_k, const void* v,
+                         int64_t ld_v, hipStream_t s) {
+        k_kv_append<KT, DT, D><<<kv_grid(c), kKvThreads, 0, s>>>(c, rot, k, ld_k, v, ld_v);
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+hipError_t launch_kv_append(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c,
+                            const RotaryArgs& rot, const void* k, int64_t ld_k, const void* v,
+                            int64_t ld_v, hipStream_t s) {
+    return by_type<AppendOp>(kt, dt, c.D, c, rot, k, ld_k, v, ld_v, s);
+}
+
+}  // namespace readme

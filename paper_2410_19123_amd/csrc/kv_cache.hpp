@@ -102,6 +102,10 @@ KvCacheArgs kv_cache_args(int64_t T, int32_t R, int32_t Hk, int32_t D, const int
 
 hipError_t launch_kv_write(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c, const void* k,
                            int64_t ld_k, const void* v, int64_t ld_v, hipStream_t s);
+struct RotaryArgs;
+hipError_t launch_kv_append(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c,
+                            const RotaryArgs& rot, const void* k, int64_t ld_k, const void* v,
+                            int64_t ld_v, hipStream_t s);
 hipError_t launch_kv_read(readme_kv_type kt, readme_dtype dt, const KvCacheArgs& c, void* k,
                           int64_t ld_k, void* v, int64_t ld_v, hipStream_t s);
 
@@ -116,6 +120,11 @@ struct KvAttnArgs {
     float score;      // log2(e) * softmax scale
     int causal;
     int64_t window;   // 0: none
+    // Rows of a draft tree, else NULL: who sees whom, and the rows' positions
+    // (NULL: those they are stored at).
+    const uint64_t* tree;
+    int64_t words;
+    const int32_t* pos;
     void* ws;
 };
 size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks);
