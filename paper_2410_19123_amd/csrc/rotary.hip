@@ -25,17 +25,9 @@ __global__ __launch_bounds__(kThreads) void k_rotary(int64_t T, int H, int D, in
     if (t >= T) return;
     const int g = (int)(tg - t * groups);
     const Chunk k = chunk_of(ch, a.rot, a.layout);
-    Turn turns[8];
-    if (k.turns) {
-        const double pos = (double)a.pos[t];
-        const float sign = a.inverse ? -1.0f : 1.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) turns[e] = turn_of(pos, a.freqs[8 * ch + e], a.amplitude, sign);
-    } else if (x == y) {
-        return;
-    }
-    for (int h0 = g; h0 < H; h0 += kBatch * groups) {
-        uint4 ra[kBatch][N], rb[kBatch][N];
+    if (!k.turns && x == y) return;
+    uint4 ra[kBatch][N], rb[kBatch][N];
+    auto load = [&](int h0) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const int h = h0 + j * groups;
@@ -44,6 +36,17 @@ __global__ __launch_bounds__(kThreads) void k_rotary(int64_t T, int H, int D, in
             load8<DT>(x, at + k.a, ra[j]);
             load8<DT>(x, at + k.b, rb[j]);
         }
+    };
+    load(g);  // on their way while the angles are computed
+    Turn turns[8];
+    if (k.turns) {
+        const double pos = (double)a.pos[t];
+        const float sign = a.inverse ? -1.0f : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turns[e] = turn_of(pos, a.freqs[8 * ch + e], a.amplitude, sign);
+    }
+    for (int h0 = g; h0 < H; h0 += kBatch * groups) {
+        if (h0 != g) load(h0);
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const int h = h0 + j * groups;
