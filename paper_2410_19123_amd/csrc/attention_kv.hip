@@ -29,7 +29,8 @@ __global__ __launch_bounds__(256) void k_attention_join(KvAttnArgs a, const int6
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     if (p.blocks > 0) {
         const int64_t share = plan[0];
-        const int64_t s = plan[1 + r] + (tl * a.c.Hk + h) * (p.blocks + kPairCost) + kPairCost;
+        const int64_t s = plan[1 + r] + kv_pair_index<ROWS>(tl, h, p.tiles, a.c.Hk) * (p.blocks + kPairCost) +
+                          kPairCost;
         const int64_t g0 = s / share, g1 = (s + p.blocks - 1) / share;
         if (g0 == g1) return;
         // Workgroup g's part is its second where the pair's first block is in
@@ -83,6 +84,7 @@ hipError_t join_of(const KvAttnArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_join(const KvAttnArgs& a, int rows, hipStream_t s) {
+    if (rows == kTreeTile) return a.c.D == 64 ? join_of<64, kTreeTile>(a, s) : join_of<128, kTreeTile>(a, s);
     switch (a.c.D) {
         case 64: return rows == kRowsTile ? join_of<64, kRowsTile>(a, s) : join_of<64, kTilesTile>(a, s);
         case 128: return rows == kRowsTile ? join_of<128, kRowsTile>(a, s) : join_of<128, kTilesTile>(a, s);
@@ -134,28 +136,49 @@ Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks)
     return {kTilesTile, tile_pairs >= 384 || blocks <= 16 ? 1 : 0};
 }
 
+// The same for rows of draft trees.
+Form tree_form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks) {
+    if (D == 256) return form_of(T, R, G, Hk, D, blocks);  // 32 rows a wave do not fit the registers
+    const int64_t rows = T * G;
+    if (blocks > 64) {
+        if (rows <= R * 16) return {kRowsTile, 0};
+        return {rows <= R * 64 ? kTreeTile : kTilesTile, 0};
+    }
+    const int tile = rows >= R * 96 ? kTreeTile : kRowsTile;
+    const int64_t pairs = (rows + tile - 1) / tile * Hk;
+    int w = 1;
+    while (w < 8 && w * 4 <= blocks && pairs * w <= (w == 4 ? 1024 : 2560)) w *= 2;
+    return {tile, w};
+}
+
 // The form of a call.  A request's rows, at most T, lie one after the other, so a
 // window bounds the blocks that any of them sees.
-Form form_of_call(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t max_blocks, int64_t window) {
+Form form_of_call(bool tree, int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t max_blocks,
+                  int64_t window) {
     int64_t blocks = max_blocks;
     if (window > 0 && (window + T) / kKvBlock + 2 < blocks) blocks = (window + T) / kKvBlock + 2;
-    return form_of(T, R, G, Hk, D, blocks);
+    return tree ? tree_form_of(T, R, G, Hk, D, blocks) : form_of(T, R, G, Hk, D, blocks);
 }
 
 }  // namespace
 
 // Enough for any window: one that bounds the blocks turns shares into whole pairs,
 // never the other way.
-size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks) {
-    const Form f = form_of(T, R, H / Hk, Hk, D, max_blocks);
-    const int64_t grid = f.waves ? 0 : f.rows == kTilesTile ? kTilesShares : kRowsShares;
+size_t kv_attention_workspace(bool tree, int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks) {
+    const Form f = form_of_call(tree, T, R, H / Hk, Hk, D, max_blocks, 0);
+    const int64_t grid = f.waves ? 0
+                         : f.rows == kTilesTile ? kTilesShares
+                         : f.rows == kTreeTile  ? kTreeShares
+                                                : kRowsShares;
     return (size_t)(kv_plan_bytes(R) + 2 * grid * f.rows * (D + 3) * 4);
 }
 
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s) {
-    const Form f = form_of_call(a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, a.c.max_blocks, a.window);
+    const Form f = form_of_call(a.tree != nullptr, a.c.T, a.c.R, a.G, a.c.Hk, a.c.D, a.c.max_blocks, a.window);
     hipError_t e;
-    if (a.tree)
+    if (f.rows == kTreeTile)
+        e = launch_attention_tree(kt, a, f.waves, s);
+    else if (a.tree)
         e = f.rows == kTilesTile ? launch_attention_tree_tiles(kt, a, f.waves == 0, s)
                                  : launch_attention_tree_rows(kt, a, f.waves, s);
     else
@@ -171,6 +194,12 @@ hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream
 // takes a whole pair (1 for tiles), 0 where shares are dealt.
 extern "C" int32_t readme_internal_attention_kv_form(int64_t T, int32_t R, int32_t H, int32_t Hk,
                                                      int32_t D, int64_t max_blocks, int64_t window) {
-    const readme::Form f = readme::form_of_call(T, R, H / Hk, Hk, D, max_blocks, window);
+    const readme::Form f = readme::form_of_call(false, T, R, H / Hk, Hk, D, max_blocks, window);
+    return f.rows * 256 + f.waves;
+}
+// The same of readme_attention_kv_tree.
+extern "C" int32_t readme_internal_attention_kv_tree_form(int64_t T, int32_t R, int32_t H, int32_t Hk,
+                                                          int32_t D, int64_t max_blocks, int64_t window) {
+    const readme::Form f = readme::form_of_call(true, T, R, H / Hk, Hk, D, max_blocks, window);
     return f.rows * 256 + f.waves;
 }

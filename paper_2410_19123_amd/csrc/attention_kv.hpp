@@ -159,56 +159,6 @@ __device__ __forceinline__ float score_offset(float log_r, float m) {
     return log_r + kUp - (m == -INFINITY ? 0.0f : m);
 }
 
-// Rows of a draft tree: row t of the request sees the tokens [lo, first) and of the
-// request's own rows, at first .. len - 1, those of its bits.  Blocks that all rows
-// see whole, between their largest lo and first, ask for no bits; word 0 of them is
-// loaded with the row.
-struct TreeRow {
-    const uint64_t* bits;
-    uint64_t word0;
-    int lo, first;
-
-    // t < 0: there is no row, and no token is seen.
-    __device__ __forceinline__ void set(const KvAttnArgs& a, int64_t row0, int n, int len, int64_t t) {
-        const int64_t f = (int64_t)len - n;
-        first = (int)f;
-        lo = first < 0 ? 0 : first;
-        bits = a.tree + (row0 + (t < 0 ? 0 : t)) * a.words;
-        word0 = 0;
-        if (t < 0) return;
-        word0 = bits[0];
-        int64_t l = 0;
-        if (a.window > 0) {
-            const int64_t p = a.pos ? (int64_t)a.pos[row0 + t] : f + t;
-            l = (p < f ? f : p) - a.window + 1;
-        }
-        lo = (int)(l < 0 ? 0 : (l < lo ? l : lo));
-    }
-    __device__ __forceinline__ uint64_t word(const KvAttnArgs& a, int i) const {
-        return i == 0 ? word0 : (i < a.words ? bits[i] : 0);
-    }
-    // Bit s: the row sees token j0 + s.
-    __device__ __forceinline__ uint64_t seen(const KvAttnArgs& a, int j0, int len) const {
-        const int l = lo - j0, f = first - j0, e = len - j0;
-        uint64_t m = ones_below(f) & ~ones_below(l);
-        if (f < kKvBlock) {
-            uint64_t own;
-            if (f > 0) {
-                own = word0 << f;
-            } else {
-                const int w = -f >> 6, sh = -f & 63;
-                own = word(a, w) >> sh;
-                if (sh) own |= word(a, w + 1) << (64 - sh);
-            }
-            m |= own & ones_below(e);
-        }
-        return m;
-    }
-    __device__ __forceinline__ static uint64_t ones_below(int n) {
-        return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1);
-    }
-};
-
 // A block whose key or value scale is not finite: every row that sees any of its
 // tokens becomes NaN through its sum (the factor and offset above stay finite, so
 // other rows' weights for it are 0).
@@ -284,6 +234,47 @@ __device__ __forceinline__ void row_keys(const KvAttnArgs& a, int len, int64_t p
     hi = (int)h;
 }
 
+// Rows of a draft tree: row t of the request sees the tokens [lo, first) and of the
+// request's own rows, at first .. len - 1, those of its bits.  Blocks that all rows
+// see whole, between their largest lo and first, ask for no bits.
+struct TreeRow {
+    int tok;  // -1: there is no row, and what it sees means nothing
+    int lo;
+
+    __device__ __forceinline__ void set(const KvAttnArgs& a, const KvRequest& q, int t) {
+        const int64_t first = (int64_t)q.len - q.n;
+        tok = t;
+        int64_t l = 0;
+        if (t >= 0 && a.window > 0) {
+            const int64_t p = a.pos ? (int64_t)a.pos[q.row0 + t] : first + t;
+            l = (p < first ? first : p) - a.window + 1;
+        }
+        lo = (int)(l < first ? l : first);
+        lo = lo < 0 ? 0 : lo;
+    }
+    // Bit s: the row sees token j0 + s.
+    __device__ __forceinline__ uint64_t seen(const KvAttnArgs& a, const KvRequest& q, int j0) const {
+        const int f = q.len - q.n - j0;  // the first own row in the block
+        uint64_t m = ones_below(f) & ~ones_below(lo - j0);
+        if (f < kKvBlock) {
+            const uint64_t* bits = a.tree + (q.row0 + (tok < 0 ? 0 : tok)) * a.words;
+            uint64_t own;
+            if (f > 0) {
+                own = bits[0] << f;
+            } else {
+                const int w = -f >> 6, sh = -f & 63;
+                own = w < a.words ? bits[w] >> sh : 0;
+                if (sh && w + 1 < a.words) own |= bits[w + 1] << (64 - sh);
+            }
+            m |= own & ones_below(q.len - j0);
+        }
+        return m;
+    }
+    __device__ __forceinline__ static uint64_t ones_below(int n) {
+        return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1);
+    }
+};
+
 // --- dealing the work out -------------------------------------------------------
 //
 // A pair is (request, tile of query rows, key head); its blocks are those that any
@@ -308,6 +299,29 @@ struct KvPlan {
     int tiles;
     int blocks;      // of each pair; a pair of none has no units
 };
+
+constexpr int kRowsTile = 16;     // query rows of a pair, in the two kernels
+constexpr int kTilesTile = 128;
+constexpr int kTreeTile = 32;     // and in that of draft trees
+constexpr int kRowsShares = 512;  // workgroups that shares are dealt to: two a CU
+constexpr int kTilesShares = 512;
+constexpr int kTreeShares = 512;
+
+// The order of a request's pairs, and which share a workgroup has.  The draft trees'
+// tiles are many to a head and read the same codes: they follow one another, and
+// neighbouring shares go to one of the eight dies, whose L2 then holds the codes.
+template <int ROWS>
+__host__ __device__ constexpr bool kv_tiles_first() {
+    return ROWS == kTreeTile;
+}
+template <int ROWS>
+__device__ __forceinline__ int64_t kv_pair_index(int64_t tile, int64_t h, int64_t tiles, int64_t Hk) {
+    return kv_tiles_first<ROWS>() ? h * tiles + tile : tile * Hk + h;
+}
+template <int ROWS>
+__device__ __forceinline__ int64_t kv_share_of(int64_t block, int64_t grid) {  // grid a multiple of 8
+    return kv_tiles_first<ROWS>() ? (block & 7) * (grid >> 3) + (block >> 3) : block;
+}
 
 template <int ROWS>
 __device__ __forceinline__ KvPlan kv_plan(const KvAttnArgs& a, const KvRequest& q) {
@@ -358,6 +372,7 @@ struct KvWalk {
     int h, b0, nb;     // blocks [b0, b0 + nb) of the pair's
     KvRequest q;
     KvPlan p;
+    int64_t me;        // the share's number
 
     // False if there is no share.  A share is at least `min_share` blocks, or a
     // whole pair where the longest is shorter: cutting finer costs more in parts
@@ -366,7 +381,8 @@ struct KvWalk {
     __device__ __forceinline__ bool start(const KvAttnArgs& a, int min_share, int64_t* plan,
                                           int64_t* lds) {
         const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-        const int64_t R = a.c.R, grid = gridDim.x, me = blockIdx.x;
+        const int64_t R = a.c.R, grid = gridDim.x;
+        me = kv_share_of<ROWS>(blockIdx.x, gridDim.x);
         int most = 0;  // blocks of the longest pair
         auto weight = [&](int64_t at) {
             if (at >= R) return (int64_t)0;
@@ -462,8 +478,13 @@ struct KvWalk {
             w += u1 - u0;
             b0 = u0 > kPairCost ? u0 - kPairCost : 0;
             nb = (u1 > kPairCost ? u1 - kPairCost : 0) - b0;
-            tile = pair / a.c.Hk;
-            h = (int)(pair - tile * a.c.Hk);
+            if constexpr (kv_tiles_first<ROWS>()) {
+                h = (int)(pair / p.tiles);
+                tile = pair - (int64_t)h * p.tiles;
+            } else {
+                tile = pair / a.c.Hk;
+                h = (int)(pair - tile * a.c.Hk);
+            }
             if (nb > 0) return true;
         }
         return false;
@@ -471,7 +492,7 @@ struct KvWalk {
 
     __device__ __forceinline__ bool whole() const { return nb == p.blocks; }
     // The pair begins in this share, or before it.
-    __device__ __forceinline__ int64_t part() const { return (int64_t)blockIdx.x * 2 + (b0 == 0 ? 1 : 0); }
+    __device__ __forceinline__ int64_t part() const { return me * 2 + (b0 == 0 ? 1 : 0); }
 };
 
 // Tile j of request r is slot floor(offsets[r] G / ROWS) + r + j, which needs no
@@ -538,14 +559,11 @@ __device__ __forceinline__ KvBlockRef kv_lane_ref(const KvBlockRef& b, int lane)
     return o;
 }
 
-constexpr int kRowsTile = 16;     // query rows of a pair, in the two kernels
-constexpr int kTilesTile = 128;
-constexpr int kRowsShares = 512;  // workgroups that shares are dealt to: two a CU
-constexpr int kTilesShares = 512;
 // `waves` of a workgroup that takes a whole pair (1, 2, 4, 8), or 0 for shares.
 hipError_t launch_attention_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attention_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
 // The same with a.tree.
+hipError_t launch_attention_tree(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attention_tree_rows(readme_kv_type kt, const KvAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attention_tree_tiles(readme_kv_type kt, const KvAttnArgs& a, bool shares, hipStream_t s);
 

@@ -90,9 +90,9 @@ struct RowsState {
         }
         const bool real = tok >= 0;
         if constexpr (TREE) {
-            tr.set(a, q.row0, q.n, q.len, tok);
+            tr.set(a, q, tok);
             lo = tr.lo;
-            hi = tr.first;
+            hi = q.len - q.n;
         } else {
             row_keys(a, q.len, (int64_t)q.len - q.n + (real ? tok : 0), lo, hi);
         }
@@ -137,8 +137,9 @@ struct RowsState {
 
     // The block held in kf and vf, its token 0 at position j0; `next` is the
     // block whose codes take its place.
-    __device__ __forceinline__ void block(const KvAttnArgs& a, float ks, float vs, int j0, int len,
+    __device__ __forceinline__ void block(const KvAttnArgs& a, const KvRequest& q, float ks, float vs, int j0,
                                           const uint8_t* next) {
+        const int len = q.len;
         const int qt = (threadIdx.x & 63) >> 4;
         f32x4 s[4];
 #pragma unroll
@@ -157,7 +158,7 @@ struct RowsState {
         const bool edge = j0 + kKvBlock > min_hi || j0 < max_lo;
         uint64_t seen = ~0ull;
         if constexpr (TREE)
-            if (edge) seen = tr.seen(a, j0, len);
+            if (edge) seen = tr.seen(a, q, j0);
         const bool sees = TREE ? seen != 0 : sees_block(lo, hi, j0);
         value_unit(vs, !edge || sees, vref, log_vref, acc, [](float x) {
             x = fmaxf(x, __shfl_xor(x, 16, 64));
@@ -264,7 +265,7 @@ struct RowsState {
             const int in = next(i + 1, nxt);
             // Past the last block the loads repeat it (cached, and in bounds).
             const int to = in < cnt ? nxt.blk : cur.blk;
-            block(a, cur.ks, cur.vs, (b0 + first + i * stride) * kKvBlock, q.len, codes(to));
+            block(a, q, cur.ks, cur.vs, (b0 + first + i * stride) * kKvBlock, codes(to));
             i = in;
             cur = nxt;
         }

@@ -85,9 +85,9 @@ struct TileState {
             }
         }
         if constexpr (TREE) {
-            tr.set(a, q.row0, q.n, q.len, real ? tok : -1);
+            tr.set(a, q, real ? (int)tok : -1);
             lo = tr.lo;
-            hi = tr.first;
+            hi = q.len - q.n;
         } else {
             row_keys(a, q.len, (int64_t)q.len - q.n + tok, lo, hi);
         }
@@ -117,8 +117,8 @@ struct TileState {
     }
 
     // The block whose token 0 is at position j0, K operands at kl, V at vl.
-    __device__ __forceinline__ void block(const KvAttnArgs& a, const uint8_t* kl, const uint8_t* vl,
-                                          float ks, float vs, int j0, int len) {
+    __device__ __forceinline__ void block(const KvAttnArgs& a, const KvRequest& q, const uint8_t* kl,
+                                          const uint8_t* vl, float ks, float vs, int j0) {
         if (j0 >= max_hi || j0 + kKvBlock <= min_lo) return;
         const int lane = threadIdx.x & 63, hf = lane >> 5;
         // Operands are read kAhead steps before their product, so that an LDS
@@ -157,7 +157,7 @@ struct TileState {
         const bool edge = j0 + kKvBlock > min_hi || j0 < max_lo;
         uint64_t seen = ~0ull;
         if constexpr (TREE)
-            if (edge) seen = tr.seen(a, j0, len);
+            if (edge) seen = tr.seen(a, q, j0);
         const bool sees = TREE ? seen != 0 : sees_block(lo, hi, j0);
         value_unit(vs, !edge || sees, vref, log_vref, acc,
                    [](float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); });
@@ -337,7 +337,7 @@ __device__ __forceinline__ void walk(const KvAttnArgs& a, const KvRequest& q, in
         const int in = next(i + 1, nxt);
         if (in < nb) sg.load(codes_of(nxt.blk));
         __syncthreads();
-        st.block(a, kl, vl, cur.ks, cur.vs, j0, q.len);
+        st.block(a, q, kl, vl, cur.ks, cur.vs, j0);
         i = in;
         cur = nxt;
         buf ^= 1;
@@ -405,7 +405,7 @@ hipError_t tiles_of(const KvAttnArgs& a, bool shares, hipStream_t s) {
     float* parts = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + kv_plan_bytes(a.c.R));
     if (shares) {
         k_attention_tiles<KT, D, TREE, true><<<kTilesShares, kThreads, 0, s>>>(a, plan, parts);
-    } else {
+    } else if constexpr (!TREE || D == 256) {  // draft trees of fewer dims take another kernel
         const int64_t grid = ceil_div(kv_slots(a.c.T, a.c.R, a.G, kTilesTile), a.c.R) * a.c.R * a.c.Hk;
         k_attention_tiles<KT, D, TREE, false><<<(unsigned)grid, kThreads, 0, s>>>(a, plan, parts);
     }

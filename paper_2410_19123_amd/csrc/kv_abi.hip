@@ -98,7 +98,7 @@ readme_status attention_args(readme_kv_type kt, int64_t T, int32_t R, int32_t H,
                              int32_t D, const void* q, int64_t ld_q, const int32_t* offsets,
                              const int32_t* lens, const int32_t* table, int64_t max_blocks,
                              int64_t n_blocks, const void* codes, const float* scales, float score,
-                             int64_t window, void* o, int64_t ld_o, void* workspace,
+                             int64_t window, void* o, int64_t ld_o, bool tree, void* workspace,
                              size_t workspace_bytes, KvAttnArgs* a, bool* done) {
     readme_status st = kv_check_attention(kt, T, R, H, Hk, D, max_blocks, n_blocks, done);
     if (st != README_OK || *done) return st;
@@ -108,7 +108,7 @@ readme_status attention_args(readme_kv_type kt, int64_t T, int32_t R, int32_t H,
     if ((st = check_rows(q, ld_q, width, 2)) != README_OK) return st;
     if ((st = check_rows(o, ld_o, width, 2)) != README_OK) return st;
     if (!workspace || !al(workspace, 16)) return README_ERR_ARG;
-    if (workspace_bytes < kv_attention_workspace(T, R, H, Hk, D, max_blocks))
+    if (workspace_bytes < kv_attention_workspace(tree, T, R, H, Hk, D, max_blocks))
         return README_ERR_WORKSPACE;
     a->q = reinterpret_cast<const uint16_t*>(q);
     a->ld_q = ld_q;
@@ -205,7 +205,7 @@ size_t readme_attention_kv_workspace_bytes(int64_t T, int32_t R, int32_t H, int3
     bool done;
     if (kv_check_attention(README_KV_I8, T, R, H, Hk, D, max_blocks, 1, &done) != README_OK || done)
         return 0;
-    return kv_attention_workspace(T, R, H, Hk, D, max_blocks);
+    return kv_attention_workspace(false, T, R, H, Hk, D, max_blocks);
 }
 
 readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32_t H, int32_t Hk,
@@ -222,7 +222,7 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
     bool done;
     const readme_status st =
         attention_args(kt, T, R, H, Hk, D, q, ld_q, offsets, lens, table, max_blocks, n_blocks, codes,
-                       scales, score, window, o, ld_o, workspace, workspace_bytes, &a, &done);
+                       scales, score, window, o, ld_o, false, workspace, workspace_bytes, &a, &done);
     if (st != README_OK || done) return st;
     a.causal = causal;
     return st_of(launch_kv_attention(kt, a, as_stream(stream)));
@@ -230,7 +230,10 @@ readme_status readme_attention_kv(readme_kv_type kt, int64_t T, int32_t R, int32
 
 size_t readme_attention_kv_tree_workspace_bytes(int64_t T, int32_t R, int32_t H, int32_t Hk,
                                                 int32_t D, int64_t max_blocks) {
-    return readme_attention_kv_workspace_bytes(T, R, H, Hk, D, max_blocks);
+    bool done;
+    if (kv_check_attention(README_KV_I8, T, R, H, Hk, D, max_blocks, 1, &done) != README_OK || done)
+        return 0;
+    return kv_attention_workspace(true, T, R, H, Hk, D, max_blocks);
 }
 
 readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, int32_t H,
@@ -249,7 +252,7 @@ readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, 
     bool done;
     const readme_status st =
         attention_args(kt, T, R, H, Hk, D, q, ld_q, offsets, lens, table, max_blocks, n_blocks, codes,
-                       scales, score, window, o, ld_o, workspace, workspace_bytes, &a, &done);
+                       scales, score, window, o, ld_o, true, workspace, workspace_bytes, &a, &done);
     if (st != README_OK || done) return st;
     if (!tree || !al(tree, 8) || !al(pos, 4)) return README_ERR_ARG;
     a.tree = tree;

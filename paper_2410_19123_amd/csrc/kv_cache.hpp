@@ -127,7 +127,7 @@ struct KvAttnArgs {
     const int32_t* pos;
     void* ws;
 };
-size_t kv_attention_workspace(int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks);
+size_t kv_attention_workspace(bool tree, int64_t T, int64_t R, int H, int Hk, int D, int64_t max_blocks);
 hipError_t launch_kv_attention(readme_kv_type kt, const KvAttnArgs& a, hipStream_t s);
 
 }  // namespace readme

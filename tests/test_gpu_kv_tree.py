@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import drafts as od
-from tests.kv_forms import SIZES, WINDOWS, kind
+from tests.kv_forms import SIZES, WINDOWS, Size
 from tests.test_gpu_kv import KT, _i32, _offsets, _poison_unused, _random_cache
 
 pytestmark = pytest.mark.gpu
@@ -63,19 +63,57 @@ def _attend(c, new, lens, H, masks, words=None, pos=None, window=0, pad=0, q=Non
     return got, o
 
 
+def form(s, D, window=0):
+    """The form that the library takes: query rows of a pair / waves to a whole
+    pair, 0 where shares are dealt."""
+    import ctypes
+    fn = _lib().load().readme_internal_attention_kv_tree_form
+    fn.restype = ctypes.c_int32
+    fn.argtypes = [ctypes.c_int64] + [ctypes.c_int32] * 4 + [ctypes.c_int64] * 2
+    rows, waves = divmod(fn(sum(s.new), len(s.new), s.Hk * s.G, s.Hk, D, s.max_blocks, window), 256)
+    return f"{rows}/{waves}"
+
+
+_FEW, _MORE = [8, 3, 0, 5], [40, 30, 0, 65]
+# Sizes named after the form that heads of up to 128 take at them; others of the
+# plain call's, which reach the same forms and those of heads of 256.
+TREES = {
+    "16/1": Size(_FEW, [100, 3, 9, 128], 3, 2, 2), "16/2": Size(_FEW, [300, 2, 9, 191], 3, 2, 5),
+    "16/4": Size(_FEW, [600, 64, 9, 450], 2, 3, 10), "16/8": Size(_FEW, [1100, 577, 0, 70], 2, 3, 18),
+    "16/0": Size(_FEW, [1100, 64, 2, 450], 2, 2, 66), "32/1": Size(_MORE, [100, 30, 9, 128], 2, 4, 2),
+    "32/2": Size(_MORE, [300, 22, 9, 191], 2, 4, 5), "32/4": Size(_MORE, [600, 94, 9, 450], 2, 4, 10),
+    "32/8": Size(_MORE, [900, 577, 0, 70], 1, 5, 18), "32/0": Size(_MORE, [900, 64, 2, 450], 2, 1, 66),
+    "128/0": Size(_MORE, [900, 64, 2, 450], 1, 3, 66),
+    "16/1 of 300": Size([2, 0, 5, 1] * 75, [70, 1, 100, 64] * 75, 2, 2, 2),
+    "32/0 of 70": Size([9, 0, 21, 13, 40] * 14, [70, 1, 100, 64, 150] * 14, 1, 2, 70),
+}
+
+
+def _size(name):
+    return TREES.get(name) or SIZES[name]
+
+
 def _sizes():
-    for name in SIZES:
+    for name in TREES:
         yield name, "e4m3", 128
-    for name in ("rows/1", "rows/4", "rows/0", "tiles/1", "tiles/0"):
-        yield name, "i8", 64
+        if " " not in name:
+            yield name, "i8", 64
+    for name in ("rows/1", "rows/8", "rows/0 of 300", "tiles/1", "tiles/0"):
+        yield name, "i8", 128
     for name in ("rows/2", "rows/0", "tiles/1", "tiles/0"):
         yield name, "i8", 256
+
+
+@pytest.mark.parametrize("name", TREES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_sizes_take_the_form_they_are_named_after(name, D):
+    assert form(TREES[name], D) == name.split()[0]
 
 
 @pytest.mark.parametrize("what", ["tree", "random", "nothing"])
 @pytest.mark.parametrize("name,kt,D", _sizes())
 def test_every_form(name, kt, D, what):
-    s = SIZES[name]
+    s = _size(name)
     c = s.cache(_random_cache, kt, D, 90)
     _poison_unused(c, s.lens)
     got, _ = _attend(c, s.new, s.lens, s.Hk * s.G, _masks(c.rng, s.new, what), pad=2)
@@ -87,20 +125,20 @@ def test_every_form(name, kt, D, what):
 
 
 @pytest.mark.parametrize("given", [False, True])
-@pytest.mark.parametrize("name,kt,D", [(n, k, d) for n, k, d in _sizes() if n in WINDOWS])
+@pytest.mark.parametrize("name,kt,D", [(n, k, d) for n, k, d in _sizes() if n in WINDOWS or n in TREES])
 def test_windows(name, kt, D, given):
     """Positions of the stored rows and given ones, below the first row and far
     above it among them."""
-    s = SIZES[name]
+    s = _size(name)
     c = s.cache(_random_cache, kt, D, 91)
     _poison_unused(c, s.lens)
-    pos = None
+    window, pos = WINDOWS.get(name, 45), None
     if given:
         first = np.concatenate([np.full(n, ln - n) for n, ln in zip(s.new, s.lens)])
         pos = first + c.rng.integers(-9, 60, len(first))
         pos[::17] = 2 ** 31 - 1
         pos[5::19] = -2 ** 31
-    _attend(c, s.new, s.lens, s.Hk * s.G, _masks(c.rng, s.new), window=WINDOWS[name], pos=pos, pad=1)
+    _attend(c, s.new, s.lens, s.Hk * s.G, _masks(c.rng, s.new), window=window, pos=pos, pad=1)
 
 
 @pytest.mark.parametrize("D,Hk,G", [(64, 2, 1), (64, 1, 7), (128, 2, 4), (256, 1, 3)])
