@@ -11,7 +11,8 @@ namespace readme {
 
 namespace {
 
-// The call's key rows, turned.
+// The call's key rows, turned.  The angles' frequencies and the row's position are
+// on their way with the row.
 template <int DT>
 struct TurnedRows {
     static constexpr int kType = README_F32;
@@ -19,20 +20,33 @@ struct TurnedRows {
     static constexpr int N = DT == README_F32 ? 2 : 1;
     struct Raw {
         uint4 a[N], b[N];
+        int pos;
     };
     const void* base;
     int64_t ld;
     RotaryArgs rot;
+    double f[8];  // of the thread's pairs
 
+    __device__ __forceinline__ TurnedRows(const void* k, int64_t ld_k, const RotaryArgs& r, int ch)
+        : base(k), ld(ld_k), rot(r) {
+        if (chunk(ch).turns) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = rot.freqs[8 * ch + e];
+        }
+    }
     __device__ __forceinline__ Chunk chunk(int ch) const { return chunk_of(ch, rot.rot, rot.layout); }
     __device__ __forceinline__ void zero(Raw& x) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) x.a[i] = x.b[i] = make_uint4(0u, 0u, 0u, 0u);
+        x.pos = 0;
     }
-    __device__ __forceinline__ void load(Raw& x, int64_t tok, int col, int ch) const {
+    __device__ __forceinline__ void load(Raw& x, const Touched& b, int row, int col, int ch) const {
         const Chunk k = chunk(ch);
-        load8<DT>(base, tok * ld + col + k.a, x.a);
-        load8<DT>(base, tok * ld + col + k.b, x.b);
+        const int64_t at = (b.tok + row) * ld + col;
+        load8<DT>(base, at + k.a, x.a);
+        load8<DT>(base, at + k.b, x.b);
+        // A stored position fits 32 bits unless its block is absent
+        x.pos = rot.pos ? rot.pos[b.tok + row] : (int)(b.j * kKvBlock + b.slot + row);
     }
     // Row `row` of the block's rows; zeros past the last.
     __device__ __forceinline__ Row16<README_F32> value(const Raw& x, const Touched& b, int row, int ch) const {
@@ -40,11 +54,9 @@ struct TurnedRows {
         widen8<DT>(x.a, v);
         widen8<DT>(x.b, v + 8);
         if (chunk(ch).turns && row < b.n) {
-            const double pos = rot.pos ? (double)rot.pos[b.tok + row]
-                                       : (double)(b.j * kKvBlock + b.slot + row);
             Turn t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] = turn_of(pos, rot.freqs[8 * ch + e], rot.amplitude, 1.0f);
+            for (int e = 0; e < 8; ++e) t[e] = turn_of((double)x.pos, f[e], rot.amplitude, 1.0f);
             turn_chunk(t, rot.layout, v);
         }
         Row16<README_F32> o;
@@ -57,17 +69,26 @@ struct TurnedRows {
 };
 
 template <int KT, int DT, int D>
-__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvCacheArgs c, RotaryArgs rot,
+__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvCacheArgs c, RotaryArgs rot, bool apart,
                                                           const void* __restrict__ k, int64_t ld_k,
                                                           const void* __restrict__ v, int64_t ld_v) {
-    write_candidate<KT, D>(c, TurnedRows<DT>{k, ld_k, rot}, PlainRows<DT>{v, ld_v});
+    write_candidate<KT, D>(c, apart, TurnedRows<DT>(k, ld_k, rot, threadIdx.x % (D / 16)),
+                           PlainRows<DT>{v, ld_v});
 }
+
+// Whether second blocks are candidates of their own.  R Hk 2 workgroups more, most of
+// them with nothing to do, against up to 32 blocks one after the other: 17 requests of
+// 5 to 33 rows, 3 heads, 7 us for 14; 300 of 2 rows, 8 heads, 28 for 13.
+bool second_apart(const KvCacheArgs& c) { return c.T > c.R && c.R * c.Hk <= 256; }
 
 template <int KT, int DT, int D>
 struct AppendOp {
     static hipError_t go(KvCacheArgs c, RotaryArgs rot, const void* k, int64_t ld_k, const void* v,
                          int64_t ld_v, hipStream_t s) {
-        k_kv_append<KT, DT, D><<<kv_grid(c), kKvThreads, 0, s>>>(c, rot, k, ld_k, v, ld_v);
+        const bool apart = second_apart(c);
+        dim3 grid = kv_grid(c);
+        if (apart) grid.x += (unsigned)c.R;
+        k_kv_append<KT, DT, D><<<grid, kKvThreads, 0, s>>>(c, rot, apart, k, ld_k, v, ld_v);
         return hipGetLastError();
     }
 };

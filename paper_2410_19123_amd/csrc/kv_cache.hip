@@ -37,7 +37,7 @@ template <int KT, int DT, int D>
 __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCacheArgs c, const void* __restrict__ k,
                                                          int64_t ld_k, const void* __restrict__ v,
                                                          int64_t ld_v) {
-    write_candidate<KT, D>(c, PlainRows<DT>{k, ld_k}, PlainRows<DT>{v, ld_v});
+    write_candidate<KT, D>(c, false, PlainRows<DT>{k, ld_k}, PlainRows<DT>{v, ld_v});
 }
 
 template <int KT, int DT, int D, bool V>
@@ -122,9 +122,9 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_read(KvCacheArgs c, void* __r
     __shared__ uint32_t lds[kKvBlock * kv_lds_row(D)];
     const int h = blockIdx.y;
     if (blockIdx.z)
-        for_touched(c, blockIdx.x, [&](const Touched& b) { read_block<KT, DT, D, true>(c, b, h, v, ld_v, lds); });
+        for_touched(c, blockIdx.x, false, [&](const Touched& b) { read_block<KT, DT, D, true>(c, b, h, v, ld_v, lds); });
     else
-        for_touched(c, blockIdx.x, [&](const Touched& b) { read_block<KT, DT, D, false>(c, b, h, k, ld_k, lds); });
+        for_touched(c, blockIdx.x, false, [&](const Touched& b) { read_block<KT, DT, D, false>(c, b, h, k, ld_k, lds); });
 }
 
 template <int KT, int DT, int D>

@@ -207,17 +207,25 @@ __device__ __forceinline__ Touched touched(const KvCacheArgs& c, int64_t r, int6
 
 // Calls f(Touched) for every block of candidate `cand` (uniform over the
 // wave): cand < R the first block of request cand, else the blocks that begin
-// at rows 64 (cand - R) .. + 63 and are not their request's first.
+// at rows 64 (cand - R) .. + 63 and are not their request's first.  With `apart` a
+// request's second block is a candidate of its own too, after the R first ones: of
+// requests of fewer than 64 rows several begin one within a run of 64 rows and would
+// follow one another, while of third and later blocks a run has at most one.
 template <class F>
-__device__ __forceinline__ void for_touched(const KvCacheArgs& c, int64_t cand, F&& f) {
-    if (cand < c.R) {
+__device__ __forceinline__ void for_touched(const KvCacheArgs& c, int64_t cand, bool apart, F&& f) {
+    const int64_t alone = apart ? 2 * c.R : c.R;
+    if (cand < alone) {
+        const bool second = cand >= c.R;
+        const int64_t r = second ? cand - c.R : cand;
         int64_t lo, hi;
-        kv_rows(c.offsets, c.T, cand, lo, hi);
-        if (lo < hi) f(touched(c, cand, lo, hi, lo));
+        kv_rows(c.offsets, c.T, r, lo, hi);
+        int64_t tok = lo;
+        if (second) tok += kKvBlock - kv_slot((int64_t)c.lens[r] - (hi - lo));
+        if (tok < hi) f(touched(c, r, lo, hi, tok));
         return;
     }
     const int lane = threadIdx.x & 63;
-    const int64_t t0 = (cand - c.R) * kKvBlock;
+    const int64_t t0 = (cand - alone) * kKvBlock;
     const int64_t t1 = t0 + kKvBlock < c.T ? t0 + kKvBlock : c.T;
     for (int64_t r0 = kv_request_at(c.offsets, c.R, t0); r0 < c.R; r0 += 64) {
         // Lane l looks at request r0 + l: does a block of it begin in the run?
@@ -225,7 +233,7 @@ __device__ __forceinline__ void for_touched(const KvCacheArgs& c, int64_t cand, 
         if (r0 + lane < c.R) {
             kv_rows(c.offsets, c.T, r0 + lane, lo, hi);
             const int64_t p = (int64_t)c.lens[r0 + lane] - (hi - lo);
-            int64_t b = lo + kKvBlock - kv_slot(p);
+            int64_t b = lo + (apart ? 2 : 1) * kKvBlock - kv_slot(p);
             if (b < t0) b += (t0 - b + kKvBlock - 1) / kKvBlock * kKvBlock;
             if (b < t1 && b < hi) tok = b;
         }
@@ -241,6 +249,9 @@ __device__ __forceinline__ void for_touched(const KvCacheArgs& c, int64_t cand, 
 }
 
 constexpr int kKvThreads = 256;
+// Passes over a block's 64 rows.
+template <int D>
+constexpr int kKvPasses = kKvBlock * (D / 16) / kKvThreads;
 // LDS holds a block's V codes as 64 token rows, one dword apart so that a
 // column's dwords spread over the banks.
 constexpr int kv_lds_row(int D) { return D / 4 + 1; }
@@ -281,8 +292,8 @@ struct PlainRows {
     const void* base;
     int64_t ld;
     __device__ __forceinline__ void zero(Raw& x) const { x.zero(); }
-    __device__ __forceinline__ void load(Raw& x, int64_t tok, int col, int ch) const {
-        x.load(base, tok * ld + col + ch * 16);
+    __device__ __forceinline__ void load(Raw& x, const Touched& b, int row, int col, int ch) const {
+        x.load(base, (b.tok + row) * ld + col + ch * 16);
     }
     __device__ __forceinline__ Row16<DT> value(const Raw& x, const Touched&, int, int) const { return x; }
 };
@@ -298,7 +309,7 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
     const int tid = threadIdx.x, lane = tid & 63;
     constexpr int LPR = D / 16;           // threads per row
     constexpr int RPP = kKvThreads / LPR;   // rows per pass
-    constexpr int NP = kKvBlock / RPP;
+    constexpr int NP = kKvPasses<D>;
     const int ch = tid % LPR, rw = tid / LPR;
     const int64_t unit = (blk * c.Hk + h) * 2 + (V ? 1 : 0);
     uint8_t* dst = c.codes + unit * kv_half_bytes(D);
@@ -310,7 +321,7 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         src.zero(raw[p]);
-        if (p * RPP + rw < b.n) src.load(raw[p], b.tok + p * RPP + rw, h * D, ch);
+        if (p * RPP + rw < b.n) src.load(raw[p], b, p * RPP + rw, h * D, ch);
     }
 #pragma unroll
     for (int p = 0; p < NP; ++p) x[p] = src.value(raw[p], b, p * RPP + rw, ch);
@@ -425,16 +436,16 @@ __device__ __forceinline__ void write_block(const KvCacheArgs& c, const Touched&
 
 // K (z = 0) or V of candidate blockIdx.x, head blockIdx.y.
 template <int KT, int D, class KRows, class VRows>
-__device__ __forceinline__ void write_candidate(const KvCacheArgs& c, const KRows& k, const VRows& v) {
+__device__ __forceinline__ void write_candidate(const KvCacheArgs& c, bool apart, KRows k, VRows v) {
     __shared__ uint32_t lds[kKvBlock * kv_lds_row(D)];
     __shared__ uint32_t most[4];
     const int h = blockIdx.y;
     if (blockIdx.z)
-        for_touched(c, blockIdx.x, [&](const Touched& b) {
+        for_touched(c, blockIdx.x, apart, [&](const Touched& b) {
             write_block<KT, D, true>(c, b, h, v, lds, most);
         });
     else
-        for_touched(c, blockIdx.x, [&](const Touched& b) {
+        for_touched(c, blockIdx.x, apart, [&](const Touched& b) {
             write_block<KT, D, false>(c, b, h, k, lds, most);
         });
 }
