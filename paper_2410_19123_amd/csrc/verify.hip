@@ -5,10 +5,13 @@
 // the first wave then walks down the tree by itself until a draft is refused or none
 // is left.  Only a refused draft asks for the whole distributions, to know what is
 // left of the target's (W), and the end for the place of the next token.  t is not
-// stored: refusals at one node change it by t = max(t - a q, 0) with an `a` each, so
-// it is computed again from p and q wherever it is read.
+// stored: as q >= 0, the refusals at a node, t = max(t - a q, 0) with an `a` each,
+// come to t = max(p - A q, 0) with A the sum of their a, so it is computed from p and
+// q wherever it is read.
 // A workgroup's waves hold a part of the vocabulary each; a pass leaves the parts'
-// sums, from which the end knows the part that holds the next token.
+// sums, from which the end knows the part that holds the next token.  What loses one
+// token by a refusal, the sum of q without the refused or, of certain drafts, t
+// itself, is summed anew in the part that held it alone.
 #include <limits.h>
 
 #include "common.hpp"
@@ -42,94 +45,157 @@ __device__ __forceinline__ double entry(const void* base, int64_t at) {
     return positive(__uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[at] << 16));
 }
 
-// Consecutive entries of a row, 16 bytes of them, as they are stored.
+// Consecutive entries of a row, 16 bytes of them, as they are stored; fewer, and zeros,
+// at the row's end, past which nothing is read.
 template <int DT>
 constexpr int kRun = DT == README_F32 ? 4 : 8;
 template <int DT>
-__device__ __forceinline__ uint4 load_run(const void* row, int64_t v, int64_t end) {
-    const char* at = reinterpret_cast<const char*>(row) + v * (16 / kRun<DT>);
-    if (v + kRun<DT> <= end) return *reinterpret_cast<const uint4*>(at);
+__device__ __forceinline__ uint4 load_run(const void* row, int64_t v) {
+    return *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) + v * (16 / kRun<DT>));
+}
+template <int DT>
+__device__ __forceinline__ uint4 load_tail(const void* row, int64_t v, int n) {
     uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int e = 0; e < kRun<DT>; ++e) {
-        if (v + e >= end) break;
+        if (e >= n) break;
         if constexpr (DT == README_F32)
-            w[e] = reinterpret_cast<const uint32_t*>(at)[e];
+            w[e] = reinterpret_cast<const uint32_t*>(row)[v + e];
         else
-            w[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(at)[e] << (16 * (e & 1));
+            w[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[v + e] << (16 * (e & 1));
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <int DT>
-__device__ __forceinline__ double run_at(const uint4& r, int e) {
+__device__ __forceinline__ double run_raw(const uint4& r, int e) {
     const int d = DT == README_F32 ? e : e >> 1;
     const uint32_t w = d == 0 ? r.x : d == 1 ? r.y : d == 2 ? r.z : r.w;
-    const float x = DT == README_F32 ? __uint_as_float(w) : e & 1 ? bf16_hi(w) : bf16_lo(w);
-    return (double)fmaxf(x, 0.0f);  // a NaN gives 0
+    return (double)(DT == README_F32 ? __uint_as_float(w) : e & 1 ? bf16_hi(w) : bf16_lo(w));
+}
+template <int DT>
+__device__ __forceinline__ double run_at(const uint4& r, int e) {
+    return fmax(run_raw<DT>(r, e), 0.0);  // a NaN gives 0
 }
 
 // A request's rows, and the refusals at the node that the walk stands at.
 struct VerifyLds {
     int parent[kMaxRows], token[kMaxRows];
-    double t[kMaxRows], q[kMaxRows];   // of the draft's token at its parent
+    double p[kMaxRows], q[kMaxRows];   // of the draft's token at its parent
     float u[kMaxRows];
-    double a[kMaxRows];                // of each refusal
     int refused[kMaxRows];
-    double sums[2][kWaves], shares[kWaves];
+    double sums[2][kWaves], shares[kWaves], again[kWaves];
     int node, child, depth;            // where the walk stands, the draft refused or -1
     int found;
 };
 
-// t of the run at v after `k` refusals at its node.
-template <int DT, bool CERTAIN>
-__device__ __forceinline__ void residual(const VerifyLds& l, const uint4& p, const uint4& q, int64_t v,
-                                         int k, double (&t)[kRun<DT>]) {
+// 0 for p below 0 or NaN too.
+__device__ __forceinline__ double left_over(double p, double q, double A) { return fmax(fma(-A, q, p), 0.0); }
+
+// The run x at v without the first k refused tokens.
+template <int DT>
+__device__ __forceinline__ void without(const VerifyLds& l, const uint4& x, int64_t v, int k,
+                                        double (&y)[kRun<DT>]) {
     constexpr int E = kRun<DT>;
 #pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = run_at<DT>(p, e);
+    for (int e = 0; e < E; ++e) y[e] = run_at<DT>(x, e);
     for (int j = 0; j < k; ++j) {
-        if constexpr (CERTAIN) {
-            const int64_t x = l.refused[j] - v;
+        const int64_t at = (int64_t)l.refused[j] - v;
+        if (!__any(at >= 0 && at < E)) continue;  // for most runs of most waves
 #pragma unroll
-            for (int e = 0; e < E; ++e) t[e] = x == e ? 0.0 : t[e];
-        } else {
-            const double a = l.a[j];
+        for (int e = 0; e < E; ++e) y[e] = at == e ? 0.0 : y[e];
+    }
+}
+// t of the run at v after k refusals at its node, the sum of whose a is A.
+template <int DT, bool CERTAIN>
+__device__ __forceinline__ void residual(const VerifyLds& l, const uint4& p, const uint4& q, int64_t v,
+                                         int k, double A, double (&t)[kRun<DT>]) {
+    if constexpr (CERTAIN) {
+        without<DT>(l, p, v, k, t);
+    } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) t[e] = fmax(fma(-a, run_at<DT>(q, e), t[e]), 0.0);
-        }
+        for (int e = 0; e < kRun<DT>; ++e) t[e] = left_over(run_raw<DT>(p, e), run_at<DT>(q, e), A);
     }
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-    return x;
+// Lane i the sum over lanes 0 .. i, by the lanes' own network: within rows of 16, then
+// from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_from(double x) {
+    const int64_t b = __double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, true);
+    return x + __longlong_as_double((int64_t)(((uint64_t)hi << 32) | lo));
+}
+__device__ __forceinline__ double wave_scan(double x) {
+    x = add_from<0x111, 0xf>(x);  // row_shr:1
+    x = add_from<0x112, 0xf>(x);
+    x = add_from<0x114, 0xf>(x);
+    x = add_from<0x118, 0xf>(x);
+    x = add_from<0x142, 0xa>(x);  // row_bcast:15 into rows 1 and 3
+    return add_from<0x143, 0xc>(x);  // row_bcast:31 into rows 2 and 3
 }
 __device__ __forceinline__ double sum_of(const double (&x)[kWaves]) {
-    double s = 0.0;
+    double s[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) s += x[i];
-    return s;
+    for (int i = 4; i < kWaves; ++i) s[i & 3] += x[i];
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Calls f(v, p, q) for the lane's runs of [v0, v1): kBatch runs of p and of q are
-// on their way together.
-constexpr int kBatch = 4;
+// Calls f(v, p, q) for the lane's runs of the entries v0 .. v0 + len - 1 (one of the
+// parts, so len fits 32 bits): in steps of 64 runs at `first`, first + stride, ..; the
+// next kBatch steps are on their way meanwhile.
+constexpr int kBatch = 2;
 template <int DT, bool CERTAIN, class F>
-__device__ __forceinline__ void for_runs(const void* p, const void* q, int64_t v0, int64_t v1, F&& f) {
-    constexpr int64_t kStep = 64 * kRun<DT>;
-    for (int64_t v = v0 + (threadIdx.x & 63) * kRun<DT>; v < v1; v += kBatch * kStep) {
-        uint4 rp[kBatch], rq[kBatch];
+__device__ __forceinline__ void for_runs(const void* p, const void* q, int64_t v0, int len, int first,
+                                         int stride, F&& f) {
+    constexpr int E = kRun<DT>, B = kBatch;
+    const int full = len / E * E;
+    p = reinterpret_cast<const char*>(p) + v0 * (16 / E);
+    if constexpr (!CERTAIN) q = reinterpret_cast<const char*>(q) + v0 * (16 / E);
+    struct Batch {
+        uint4 p[B], q[B];
+    } a, b;
+    const int mine = (threadIdx.x & 63) * E;
+    // Past the last whole run the loads repeat it
+    auto fetch = [&](int at, Batch& x) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            rp[i] = rq[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (v + i * kStep >= v1) continue;
-            rp[i] = load_run<DT>(p, v + i * kStep, v1);
-            if constexpr (!CERTAIN) rq[i] = load_run<DT>(q, v + i * kStep, v1);
+        for (int i = 0; i < B; ++i) {
+            const int v = min(at + i * stride + mine, full - E);
+            const uint32_t byte = (uint32_t)v * (16 / E);
+            x.p[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + byte);
+            if constexpr (!CERTAIN) x.q[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(q) + byte);
         }
+    };
+    auto use = [&](int at, const Batch& x) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-            if (v + i * kStep < v1) f(v + i * kStep, rp[i], rq[i]);
+        for (int i = 0; i < B; ++i) {
+            const int v = at + i * stride + mine;
+            if (v < full) f(v0 + v, x.p[i], CERTAIN ? x.p[i] : x.q[i]);
+        }
+    };
+    if (first < full) {
+        fetch(first, a);
+        for (int at = first;;) {
+            const int after = at + B * stride;
+            if (after >= full) {
+                use(at, a);
+                break;
+            }
+            fetch(after, b);
+            use(at, a);
+            at = after + B * stride;
+            if (at >= full) {
+                use(after, b);
+                break;
+            }
+            fetch(at, a);
+            use(after, b);
+        }
+    }
+    // What is left of the row, by the first lane whose step it would be
+    if (full < len && (full / (64 * E)) % (stride / (64 * E)) == first / (64 * E) && mine == full % (64 * E)) {
+        const uint4 tp = load_tail<DT>(p, full, len - full);
+        f(v0 + full, tp, CERTAIN ? tp : load_tail<DT>(q, full, len - full));
     }
 }
 
@@ -137,7 +203,7 @@ template <int DT, bool CERTAIN>
 __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a) {
     constexpr int E = kRun<DT>;
     __shared__ VerifyLds l;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t r = blockIdx.x;
     int64_t lo = a.offsets[r], hi = a.offsets[r + 1];
     lo = lo < 0 ? 0 : (lo > a.T ? a.T : lo);
@@ -157,21 +223,26 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a) {
         l.parent[tid] = real ? par : -1;
         l.token[tid] = known ? x : -1;
         l.u[tid] = a.u[lo + tid];
-        l.t[tid] = known ? entry<DT>(a.p, (lo + par) * a.ld_p + x) : 0.0;
+        l.p[tid] = known ? entry<DT>(a.p, (lo + par) * a.ld_p + x) : 0.0;
         l.q[tid] = !known ? 0.0 : CERTAIN ? 1.0 : entry<DT>(a.q, (lo + par) * a.ld_q + x);
     }
     __syncthreads();
     // Each wave's part of the vocabulary, in whole steps of its lanes' runs
-    constexpr int64_t kStep = 64 * E;
-    const int64_t part = (a.V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
-    const int64_t v0 = wv * part < a.V ? wv * part : a.V, v1 = v0 + part < a.V ? v0 + part : a.V;
+    constexpr int kStep = 64 * E;
+    const int64_t part = (a.V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;  // at most 2^27 + kStep
+    const int64_t v0 = wv * part < a.V ? wv * part : a.V;
+    auto length = [&](int64_t from) { return (int)(a.V - from < part ? a.V - from : part); };
+    const int len = length(v0);
     constexpr int es = 16 / E;
     auto row_of = [&](const void* base, int64_t ld, int node) {
         return reinterpret_cast<const void*>(reinterpret_cast<const char*>(base) + (lo + node) * ld * es);
     };
 
     int node = 0, last = 0, k = 0, depth = 0;
-    double rate = 1.0, all = 0.0, gone = 0.0;  // sums of q at the node, and of its refused tokens
+    double rate = 1.0, A = 0.0;  // a, and the sum of the refusals'
+    const bool loses = CERTAIN || a.distinct;  // p or q loses the refused token
+    int pending = -1;                          // the part whose sum is `changed`
+    double changed = 0.0;
     for (;;) {
         // The first wave: on while drafts are taken
         if (wv == 0) {
@@ -183,92 +254,101 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a) {
                     const uint64_t hit = __ballot(i < n && i > last && l.parent[i] == node);
                     if (hit) child = g * 64 + __ffsll((unsigned long long)hit) - 1;
                 }
-                if (child < 0 || !((double)l.u[child] * rate * l.q[child] < l.t[child])) break;
+                if (child < 0) break;
+                double t = CERTAIN ? l.p[child] : left_over(l.p[child], l.q[child], A), qx = l.q[child];
+                if (loses) {  // a token refused before has lost its p, or q
+                    bool gone = false;
+                    for (int j = lane; j - lane < k; j += 64)
+                        gone = gone || __ballot(j < k && l.refused[j] == l.token[child]) != 0;
+                    if (gone) t = qx = 0.0;
+                }
+                if (!((double)l.u[child] * rate * qx < t)) break;
                 ++depth;
                 if (lane == 0) a.path[lo + depth] = child;
                 node = last = child;
                 k = 0;
                 rate = 1.0;
+                A = 0.0;
+                pending = -1;
             }
             if (lane == 0) {
                 l.node = node;
                 l.child = child;
                 l.depth = depth;
-                if (child >= 0) {  // the refusal that comes next
-                    l.a[k] = rate;
-                    l.refused[k] = l.token[child];
-                }
+                if (child >= 0) l.refused[k] = l.token[child];  // the refusal that comes next
             }
         }
         __syncthreads();
-        if (l.node != node || l.depth != depth) k = 0, rate = 1.0;
-        node = l.node;
-        depth = l.depth;
-        const int child = l.child;
+        if (l.depth != depth) k = 0, rate = 1.0, A = 0.0, pending = -1;
+        // The part that the last refusal changed, now that its old sum is read no more
+        if (!CERTAIN && pending >= 0 && tid == 0) l.shares[pending] = changed;
+        // The same for all lanes, and so are the rows' addresses
+        node = __builtin_amdgcn_readfirstlane(l.node);
+        depth = __builtin_amdgcn_readfirstlane(l.depth);
+        const int child = __builtin_amdgcn_readfirstlane(l.child);
         if (child < 0) break;
         last = child;
         // Refused: what is left of the target's distribution, and of the drafts'
         const void *p = row_of(a.p, a.ld_p, node), *q = CERTAIN ? nullptr : row_of(a.q, a.ld_q, node);
-        const bool first = k == 0 && !CERTAIN && a.distinct;
-        double w = 0.0, s = 0.0;
-        for_runs<DT, CERTAIN>(p, q, v0, v1, [&](int64_t v, const uint4& rp, const uint4& rq) {
-            double t[E];
-            residual<DT, CERTAIN>(l, rp, rq, v, k + 1, t);
+        const int x = __builtin_amdgcn_readfirstlane(l.token[child]);
+        const double A1 = A + rate;
+        if (!CERTAIN || k == 0) {
+            const bool first = !CERTAIN && a.distinct && k == 0;
+            double w = 0.0, s = 0.0;
+            for_runs<DT, CERTAIN>(p, q, v0, len, 0, kStep, [&](int64_t v, const uint4& rp, const uint4& rq) {
+                double t[E];
+                residual<DT, CERTAIN>(l, rp, rq, v, k + 1, A1, t);
 #pragma unroll
-            for (int e = 0; e < E; ++e) w += t[e];
+                for (int e = 0; e < E; ++e) w += t[e];
+                if (first) {
+                    without<DT>(l, rq, v, k + 1, t);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s += t[e];
+                }
+            });
+            w = wave_scan(w);
+            if (lane == 63) l.sums[(k + 1) & 1][wv] = w;
             if (first) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) s += run_at<DT>(rq, e);
+                s = wave_scan(s);
+                if (lane == 63) l.shares[wv] = s;
             }
-        });
-        w = wave_sum(w);
-        if (first) s = wave_sum(s);
-        // Not over the sums of an earlier refusal, which stay if nothing is left
-        if (lane == 0) {
-            l.sums[(k + 1) & 1][wv] = w;
-            l.shares[wv] = s;
+        } else if (lane == 63) {
+            l.sums[(k + 1) & 1][wv] = wv == pending ? changed : l.sums[k & 1][wv];
+        }
+        // Of the others only the part that held x changes: summed anew by all waves
+        const int at = loses && k > 0 && x >= 0 ? (int)(x / part) : -1;
+        if (at >= 0) {
+            double s = 0.0;
+            for_runs<DT, true>(CERTAIN ? p : q, nullptr, at * part, length(at * part), wv * kStep, kWaves * kStep,
+                               [&](int64_t v, const uint4& run, const uint4&) {
+                                   double y[E];
+                                   without<DT>(l, run, v, k + 1, y);
+#pragma unroll
+                                   for (int e = 0; e < E; ++e) s += y[e];
+                               });
+            s = wave_scan(s);
+            if (lane == 63) l.again[wv] = s;
         }
         __syncthreads();
-        w = sum_of(l.sums[(k + 1) & 1]);
-        if (first) all = sum_of(l.shares);
+        // From here to the barrier after the next walk only these sums are read
+        double part_sums[2][kWaves];
+        const double now = at >= 0 ? sum_of(l.again) : 0.0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            part_sums[0][i] = CERTAIN && i == at ? now : l.sums[(k + 1) & 1][i];
+            part_sums[1][i] = !CERTAIN && i == at ? now : l.shares[i];
+        }
+        const double w = sum_of(part_sums[0]);
         if (!(w > 0.0)) break;
-        const int x = l.token[child];
-        const double refused_q = l.q[child];
-        __syncthreads();
-        if (tid < n && l.parent[tid] == node) {
-            double t = l.t[tid];
-            if constexpr (CERTAIN) {
-                if (l.token[tid] == x) t = 0.0;
-            } else {
-                t = fmax(fma(-rate, l.q[tid], t), 0.0);
-                if (a.distinct && l.token[tid] == x) l.q[tid] = 0.0;
-            }
-            l.t[tid] = t;
-        }
-        rate = w;
-        if (!CERTAIN && a.distinct) {
-            gone = k == 0 ? refused_q : gone + refused_q;
-            s = all - gone;
-            if (s < all * 0x1p-10) {
-                // Little is left: anew, without the cancellation
-                s = 0.0;
-                for_runs<DT, true>(q, nullptr, v0, v1, [&](int64_t v, const uint4& rq, const uint4&) {
-                    double y[E];
-                    residual<DT, true>(l, rq, rq, v, k + 1, y);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) s += y[e];
-                });
-                s = wave_sum(s);
-                if (lane == 0) l.shares[wv] = s;
-                __syncthreads();
-                s = sum_of(l.shares);
-            }
-            rate = s > 0.0 ? w / s : 0.0;
-        }
+        const double s = sum_of(part_sums[1]);
+        A = A1;
+        rate = !CERTAIN && a.distinct ? (s > 0.0 ? w / s : 0.0) : w;
         ++k;
-        __syncthreads();
+        pending = at;
+        changed = now;
     }
     __syncthreads();  // the walk's last reads of l are over
+    if (pending >= 0 && CERTAIN && tid == 0) l.sums[k & 1][pending] = changed;
 
     // The next token: the parts' sums of t, the part that holds the border, and in it
     // the step, the lane and the entry.
@@ -276,12 +356,12 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a) {
     double(&sums)[kWaves] = l.sums[k & 1];
     if (k == 0) {
         double w = 0.0;
-        for_runs<DT, true>(p, nullptr, v0, v1, [&](int64_t, const uint4& rp, const uint4&) {
+        for_runs<DT, true>(p, nullptr, v0, len, 0, kStep, [&](int64_t, const uint4& rp, const uint4&) {
 #pragma unroll
             for (int e = 0; e < E; ++e) w += run_at<DT>(rp, e);
         });
-        w = wave_sum(w);
-        if (lane == 0) sums[wv] = w;
+        w = wave_scan(w);
+        if (lane == 63) sums[wv] = w;
     }
     if (tid == 0) {
         l.found = -1;
@@ -317,17 +397,16 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) t[e] = 0.0;
         if (v < p1) {
-            const uint4 rp = load_run<DT>(p, v, p1);
-            residual<DT, CERTAIN>(l, rp, CERTAIN ? rp : load_run<DT>(q, v, p1), v, k, t);
+            auto run = [&](const void* row) {
+                return v + E <= p1 ? load_run<DT>(row, v) : load_tail<DT>(row, v, (int)(p1 - v));
+            };
+            const uint4 rp = run(p);
+            const uint4 rq = CERTAIN || k == 0 ? make_uint4(0u, 0u, 0u, 0u) : run(q);
+            residual<DT, CERTAIN>(l, rp, rq, v, k, A, t);
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) mine += t[e];
-        double incl = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double y = __shfl_up(incl, off, 64);
-            if (lane >= off) incl += y;
-        }
+        const double incl = wave_scan(mine);
         __syncthreads();  // an earlier step's reads of l.shares are over
         if (lane == 63) l.shares[wv] = incl;
         __syncthreads();

@@ -153,6 +153,24 @@ def test_nothing_left():
     assert acc[0] == 0 and tok[0] >= 0
 
 
+@pytest.mark.parametrize("kind", ["given", "distinct", "certain"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_little_left_after_refusals(kind, dtype):
+    """Nearly all of both distributions lies on the tokens refused first, so that what
+    is left of them is far below what was taken away."""
+    for seed in range(6):
+        c = Case([6, 5, 6], 700, 1, kind, dtype, seed=seed)
+        c.parent[:] = 0
+        heavy = torch.tensor([[13, 699, 350], [0, 64, 512], [8, 9, 10]])
+        for r, o in enumerate((0, 6, 11)):
+            c.p[o, heavy[r]] = torch.tensor([1e3, 5e6, 2e4], device="cuda:0").to(dtype)
+            if c.q is not None:
+                c.q[o, heavy[r]] = torch.tensor([3e3, 2e7, 7e4], device="cuda:0").to(dtype)
+            c.tokens[o + 1:o + 4] = heavy[r].numpy()
+        c.u[:] = np.where(np.arange(17) % 5 == 0, 0.3, 1.0 - 2.0 ** -24)
+        c.check(safe=False)
+
+
 def test_borders_and_extreme_random_numbers():
     """Sums that are exact: a border that a sum meets belongs to the entry after it.
     0 and the number below 1 pick the first and the last entry."""
