@@ -241,12 +241,16 @@ struct TreeRow {
     int tok;  // -1: there is no row, and what it sees means nothing
     int lo;
 
-    __device__ __forceinline__ void set(const KvAttnArgs& a, const KvRequest& q, int t) {
+    // The given position, where it matters: on its way before set() asks for it.
+    __device__ __forceinline__ static int position(const KvAttnArgs& a, const KvRequest& q, int t) {
+        return t >= 0 && a.window > 0 && a.pos ? a.pos[q.row0 + t] : 0;
+    }
+    __device__ __forceinline__ void set(const KvAttnArgs& a, const KvRequest& q, int t, int given) {
         const int64_t first = (int64_t)q.len - q.n;
         tok = t;
         int64_t l = 0;
         if (t >= 0 && a.window > 0) {
-            const int64_t p = a.pos ? (int64_t)a.pos[q.row0 + t] : first + t;
+            const int64_t p = a.pos ? (int64_t)given : first + t;
             l = (p < first ? first : p) - a.window + 1;
         }
         lo = (int)(l < first ? l : first);
@@ -534,21 +538,24 @@ struct KvBlockRef {
     int blk;
     float ks, vs;
 };
+// The block's scales as they are stored, and as the kernels take them.
+__device__ __forceinline__ float2 kv_block_scales(const KvAttnArgs& a, int blk, int h) {
+    if (blk < 0) return make_float2(0.0f, 0.0f);
+    return *reinterpret_cast<const float2*>(a.c.scales + ((int64_t)blk * a.c.Hk + h) * 2);
+}
+__device__ __forceinline__ void kv_set_scales(KvBlockRef& b, float2 sc) {
+    // An infinite scale counts as NaN: its logarithm and products of a score
+    // of zero are not numbers.
+    const bool bad = bad_scales(sc.x, sc.y);
+    b.ks = bad ? __builtin_nanf("") : sc.x;
+    // No scale that the write gives is subnormal; one counts as zero, since its
+    // reciprocal is infinite.
+    b.vs = bad ? __builtin_nanf("") : sc.y < 0x1p-126f ? 0.0f : sc.y;
+}
 __device__ __forceinline__ KvBlockRef kv_block_ref(const KvAttnArgs& a, int64_t r, int64_t j, int h) {
     KvBlockRef b;
     b.blk = (int)kv_block_of(a.c.table, a.c.max_blocks, a.c.n_blocks, r, j);
-    b.ks = b.vs = 0.0f;
-    if (b.blk >= 0) {
-        const float2 sc =
-            *reinterpret_cast<const float2*>(a.c.scales + ((int64_t)b.blk * a.c.Hk + h) * 2);
-        // An infinite scale counts as NaN: its logarithm and products of a score
-        // of zero are not numbers.
-        const bool bad = bad_scales(sc.x, sc.y);
-        b.ks = bad ? __builtin_nanf("") : sc.x;
-        // No scale that the write gives is subnormal; one counts as zero, since its
-        // reciprocal is infinite.
-        b.vs = bad ? __builtin_nanf("") : sc.y < 0x1p-126f ? 0.0f : sc.y;
-    }
+    kv_set_scales(b, kv_block_scales(a, b.blk, h));
     return b;
 }
 __device__ __forceinline__ KvBlockRef kv_lane_ref(const KvBlockRef& b, int lane) {

@@ -53,6 +53,7 @@ struct RowsState {
         const int head = h * a.G + (real ? (int)i - t * a.G : 0);
         const uint16_t* row = a.q + (q.row0 + t) * a.ld_q + (int64_t)head * D;
         tok = real ? t : -1;
+        if constexpr (TREE) tr.lo = TreeRow::position(a, q, tok);  // until set() takes it
 #pragma unroll
         for (int f = 0; f < 2 * NK; ++f) {
             raw[f] = make_uint4(0u, 0u, 0u, 0u);
@@ -90,7 +91,7 @@ struct RowsState {
         }
         const bool real = tok >= 0;
         if constexpr (TREE) {
-            tr.set(a, q, tok);
+            tr.set(a, q, tok, tr.lo);
             lo = tr.lo;
             hi = q.len - q.n;
         } else {
@@ -231,19 +232,24 @@ struct RowsState {
         int tok;
         fetch(a, q, tile, h, raw, tok);
         clear();
-        // Lane i holds the number and scales of the wave's i-th of the current
-        // 64 blocks; absent blocks are stepped over.
+        // Lane i holds the number and scales of the wave's i-th of the current 64
+        // blocks; absent blocks are stepped over.
         KvBlockRef refs;
         const int cnt = first < nb ? (nb - first + stride - 1) / stride : 0;
+        auto number = [&](int i) {
+            refs.blk = -1;
+            if (i + lane < cnt)
+                refs.blk = (int)kv_block_of(a.c.table, a.c.max_blocks, a.c.n_blocks, r, b0 + first + (i + lane) * stride);
+            // Wait for them here, not wherever the paths meet again (which would
+            // wait for every code on its way as well).
+            asm volatile("" : "+v"(refs.blk));
+        };
         auto next = [&](int i, KvBlockRef& b) {
             for (; i < cnt; ++i) {
-                if ((i & 63) == 0) {
-                    refs.blk = -1;
-                    refs.ks = refs.vs = 0.0f;
-                    if (i + lane < cnt) refs = kv_block_ref(a, r, b0 + first + (i + lane) * stride, h);
-                    // Wait for them here, not wherever the paths meet again (which
-                    // would wait for every code on its way as well).
-                    asm volatile("" : "+v"(refs.blk), "+v"(refs.ks), "+v"(refs.vs));
+                if ((i & 63) == 0 && i > 0) {
+                    number(i);
+                    kv_set_scales(refs, kv_block_scales(a, refs.blk, h));
+                    asm volatile("" : "+v"(refs.ks), "+v"(refs.vs));
                 }
                 b = kv_lane_ref(refs, i & 63);
                 if (b.blk >= 0) break;
@@ -253,6 +259,11 @@ struct RowsState {
         auto codes = [&](int blk) {
             return a.c.codes + ((int64_t)blk * a.c.Hk + h) * 2 * kKvBlock * D;
         };
+        // The first codes follow their blocks' numbers at once, the scales on their
+        // way beside them: one round to memory less before the first score.
+        number(0);
+        const float2 scales = kv_block_scales(a, refs.blk, h);
+        refs.ks = refs.vs = 0.0f;
         KvBlockRef cur, nxt;
         int i = next(0, cur);
         if (i < cnt) {
@@ -260,6 +271,11 @@ struct RowsState {
             load_v(codes(cur.blk));
         }
         start(a, q, raw, tok);
+        if (i < 64) {
+            kv_set_scales(refs, scales);
+            asm volatile("" : "+v"(refs.ks), "+v"(refs.vs));
+            cur = kv_lane_ref(refs, i);
+        }
         while (i < cnt) {
             nxt = cur;
             const int in = next(i + 1, nxt);

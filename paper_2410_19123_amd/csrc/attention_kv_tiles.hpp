@@ -85,7 +85,8 @@ struct TileState {
             }
         }
         if constexpr (TREE) {
-            tr.set(a, q, real ? (int)tok : -1);
+            const int t = real ? (int)tok : -1;
+            tr.set(a, q, t, TreeRow::position(a, q, t));
             lo = tr.lo;
             hi = q.len - q.n;
         } else {

@@ -34,7 +34,7 @@ struct TreeState {
     TreeRow tr;
 
     __device__ __forceinline__ void fetch(const KvAttnArgs& a, const KvRequest& q, int64_t tile, int h,
-                                          uint4 (&raw)[NQ]) {
+                                          uint4 (&raw)[NQ], int& pos) {
         const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
         const int64_t i = tile * kRows + col;
         const bool real = i < (int64_t)q.n * a.G;
@@ -46,10 +46,13 @@ struct TreeState {
             raw[s] = make_uint4(0u, 0u, 0u, 0u);
             if (real) raw[s] = *reinterpret_cast<const uint4*>(row + (s >> 1) * 32 + hf * 16 + (s & 1) * 8);
         }
-        tr.set(a, q, real ? t : -1);
+        tr.tok = real ? t : -1;
+        pos = TreeRow::position(a, q, tr.tok);
     }
 
-    __device__ __forceinline__ void start(const KvAttnArgs& a, const uint4 (&raw)[NQ]) {
+    __device__ __forceinline__ void start(const KvAttnArgs& a, const KvRequest& q, const uint4 (&raw)[NQ],
+                                          int pos) {
+        tr.set(a, q, tr.tok, pos);
         float big = 0.0f;
 #pragma unroll
         for (int s = 0; s < NQ; ++s) {
@@ -198,20 +201,26 @@ struct TreeState {
         const int lane = threadIdx.x & 63;
         const int first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         uint4 raw[NQ];
-        fetch(a, q, tile, h, raw);
+        int pos;
+        fetch(a, q, tile, h, raw, pos);
         // Lane i holds the number and scales of the wave's i-th of the current 64
         // blocks; absent blocks are stepped over.
         KvBlockRef refs;
         const int cnt = first < nb ? (nb - first + W - 1) / W : 0;
+        auto number = [&](int i) {
+            refs.blk = -1;
+            if (i + lane < cnt)
+                refs.blk = (int)kv_block_of(a.c.table, a.c.max_blocks, a.c.n_blocks, r, b0 + first + (i + lane) * W);
+            // Wait for them here, not wherever the paths meet again (which would
+            // wait for every code on its way as well).
+            asm volatile("" : "+v"(refs.blk));
+        };
         auto next = [&](int i, KvBlockRef& b) {
             for (; i < cnt; ++i) {
-                if ((i & 63) == 0) {
-                    refs.blk = -1;
-                    refs.ks = refs.vs = 0.0f;
-                    if (i + lane < cnt) refs = kv_block_ref(a, r, b0 + first + (i + lane) * W, h);
-                    // Wait for them here, not wherever the paths meet again (which
-                    // would wait for every code on its way as well).
-                    asm volatile("" : "+v"(refs.blk), "+v"(refs.ks), "+v"(refs.vs));
+                if ((i & 63) == 0 && i > 0) {
+                    number(i);
+                    kv_set_scales(refs, kv_block_scales(a, refs.blk, h));
+                    asm volatile("" : "+v"(refs.ks), "+v"(refs.vs));
                 }
                 b = kv_lane_ref(refs, i & 63);
                 if (b.blk >= 0) break;
@@ -221,13 +230,23 @@ struct TreeState {
         auto codes = [&](int blk) {
             return a.c.codes + ((int64_t)blk * a.c.Hk + h) * 2 * kKvBlock * D;
         };
+        // The first codes follow their blocks' numbers at once, the scales on their
+        // way beside them: one round to memory less before the first score.
+        number(0);
+        const float2 scales = kv_block_scales(a, refs.blk, h);
+        refs.ks = refs.vs = 0.0f;
         KvBlockRef cur, nxt;
         int i = next(0, cur);
         if (i < cnt) {
             load_k(codes(cur.blk));
             load_v(codes(cur.blk));
         }
-        start(a, raw);
+        start(a, q, raw, pos);
+        if (i < 64) {
+            kv_set_scales(refs, scales);
+            asm volatile("" : "+v"(refs.ks), "+v"(refs.vs));
+            cur = kv_lane_ref(refs, i);
+        }
         while (i < cnt) {
             nxt = cur;
             const int in = next(i + 1, nxt);
