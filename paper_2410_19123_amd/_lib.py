@@ -977,26 +977,31 @@ def readme_rotary_freqs(rot: int, theta: float = 10000.0, scaling: int = README_
 
 def _freqs_args(freqs, dev: int) -> int:
     """rot of the frequencies."""
-    if freqs.dtype is not torch.float64 or freqs.dim() != 1:
+    size = freqs.shape
+    if freqs.dtype is not torch.float64 or len(size) != 1:
         raise ValueError("freqs must be fp64 [rot / 2]")
-    _on(dev, freqs=freqs)
-    return 2 * freqs.shape[0]
+    _on(dev, freqs, "freqs")
+    return 2 * size[0]
 
 
-def _on(dev: int, **tensors) -> None:
-    """Tensors (or None) must be contiguous, on device `dev`."""
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.get_device() != dev:
-            raise ValueError(f"{name} must be on the call's device")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+def _on(dev: int, t, name: str) -> None:
+    """A tensor (or None) must be contiguous, on device `dev`."""
+    if t is None:
+        return
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the call's device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
-def _vector(t, n: int, dtype, name: str) -> None:
-    if t is not None and (t.dtype is not dtype or t.shape != (n,)):
+def _vector(t, n: int, dtype, dev: int, name: str):
+    """The address of a vector [n] (or None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != (n,):
         raise ValueError(f"{name} must be {dtype} [{n}]")
+    _on(dev, t, name)
+    return t.data_ptr()
 
 
 def readme_rotary(x, pos, freqs, D: int, layout: int = README_ROTARY_HALF, amplitude: float = 1.0,
@@ -1016,10 +1021,9 @@ def readme_rotary(x, pos, freqs, D: int, layout: int = README_ROTARY_HALF, ampli
         raise ValueError("x and y dtypes disagree")
     ld_x, ld_y = _kv_rows(x, T, width, dev, "x"), _kv_rows(y, T, width, dev, "y")
     rot = _freqs_args(freqs, dev)
-    _vector(pos, T, torch.int32, "pos")
-    _on(dev, pos=pos)
     _kv_call(dev, "readme_rotary", _dt(x), T, width // D, D, rot, layout, 1 if inverse else 0,
-             amplitude, pos.data_ptr(), freqs.data_ptr(), x.data_ptr(), ld_x, y.data_ptr(), ld_y)
+             amplitude, _vector(pos, T, torch.int32, dev, "pos"), freqs.data_ptr(), x.data_ptr(), ld_x,
+             y.data_ptr(), ld_y)
     return y
 
 
@@ -1033,10 +1037,8 @@ def readme_kv_append(kt: int, k, v, offsets, lens, table, codes, scales, freqs, 
     if v.dtype is not k.dtype:
         raise ValueError("k and v dtypes disagree")
     rot = _freqs_args(freqs, dev)
-    _vector(pos, T, torch.int32, "pos")
-    _on(dev, pos=pos)
     _kv_call(dev, "readme_kv_append", kt, _dt(k), T, R, Hk, D, rot, layout, amplitude,
-             None if pos is None else pos.data_ptr(), freqs.data_ptr(), k.data_ptr(), ld_k,
+             _vector(pos, T, torch.int32, dev, "pos"), freqs.data_ptr(), k.data_ptr(), ld_k,
              v.data_ptr(), ld_v, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb,
              codes.data_ptr(), scales.data_ptr())
 
@@ -1060,15 +1062,15 @@ def readme_attention_kv_tree(kt: int, q, offsets, lens, table, codes, scales, H:
     ld_q, ld_o = _kv_rows(q, T, H * D, dev, "q"), _kv_rows(o, T, H * D, dev, "o")
     if tree.dtype is not torch.int64 or tree.dim() != 2 or tree.shape[0] != T:
         raise ValueError("tree must be int64 [T][words]")
-    _vector(pos, T, torch.int32, "pos")
-    _on(dev, tree=tree, pos=pos, workspace=workspace)
+    _on(dev, tree, "tree")
+    _on(dev, workspace, "workspace")
     if workspace is None:
         ws = readme_attention_kv_tree_workspace_bytes(T, R, H, Hk, D, mb)
         workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=codes.device)
     _kv_call(dev, "readme_attention_kv_tree", kt, T, R, H, Hk, D, q.data_ptr(), ld_q,
              offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), mb, nb, codes.data_ptr(),
              scales.data_ptr(), tree.data_ptr(), tree.shape[1],
-             None if pos is None else pos.data_ptr(), D ** -0.5 if scale is None else scale, window,
+             _vector(pos, T, torch.int32, dev, "pos"), D ** -0.5 if scale is None else scale, window,
              o.data_ptr(), ld_o, workspace.data_ptr(), workspace.nbytes)
     return o
 
@@ -1094,10 +1096,6 @@ def readme_verify_drafts(offsets, tokens, parent, p, q, u, distinct: bool = Fals
     path = torch.empty(T, **new) if path is None else path
     accepted = torch.empty(R, **new) if accepted is None else accepted
     token = torch.empty(R, **new) if token is None else token
-    for t, n, name in ((offsets, R + 1, "offsets"), (tokens, T, "tokens"), (parent, T, "parent"),
-                       (path, T, "path"), (accepted, R, "accepted"), (token, R, "token")):
-        _vector(t, n, i32, name)
-    _vector(u, T, torch.float32, "u")
     one = 16 // p.element_size()
     row = -(-V // one) * one  # the stride of a single row, which has none
     ld_p, ld_q = _kv_rows(p, T, V, dev, "p") if T > 1 else row, 0
@@ -1109,12 +1107,13 @@ def readme_verify_drafts(offsets, tokens, parent, p, q, u, distinct: bool = Fals
     if workspace is None:
         ws = readme_verify_drafts_workspace_bytes(T, R, V)
         workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=p.device)
-    _on(dev, offsets=offsets, tokens=tokens, parent=parent, u=u, path=path, accepted=accepted,
-        token=token, workspace=workspace)
-    _kv_call(dev, "readme_verify_drafts", _dt(p), T, R, V, offsets.data_ptr(), tokens.data_ptr(),
-             parent.data_ptr(), p.data_ptr(), ld_p, None if q is None else q.data_ptr(), ld_q,
-             u.data_ptr(), 1 if distinct else 0, path.data_ptr(), accepted.data_ptr(),
-             token.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+    _on(dev, workspace, "workspace")
+    _kv_call(dev, "readme_verify_drafts", _dt(p), T, R, V, _vector(offsets, R + 1, i32, dev, "offsets"),
+             _vector(tokens, T, i32, dev, "tokens"), _vector(parent, T, i32, dev, "parent"),
+             p.data_ptr(), ld_p, None if q is None else q.data_ptr(), ld_q,
+             _vector(u, T, torch.float32, dev, "u"), 1 if distinct else 0,
+             _vector(path, T, i32, dev, "path"), _vector(accepted, R, i32, dev, "accepted"),
+             _vector(token, R, i32, dev, "token"), workspace.data_ptr(), workspace.nbytes)
     return path, accepted, token
 
 
