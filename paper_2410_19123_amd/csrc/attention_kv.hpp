@@ -253,8 +253,8 @@ struct TreeRow {
             const int64_t p = a.pos ? (int64_t)given : first + t;
             l = (p < first ? first : p) - a.window + 1;
         }
-        lo = (int)(l < first ? l : first);
-        lo = lo < 0 ? 0 : lo;
+        l = l < first ? l : first;
+        lo = (int)(l < 0 ? 0 : l);  // a wide window leaves l far below 32 bits
     }
     // Bit s: the row sees token j0 + s.
     __device__ __forceinline__ uint64_t seen(const KvAttnArgs& a, const KvRequest& q, int j0) const {

@@ -141,6 +141,19 @@ def test_windows(name, kt, D, given):
     _attend(c, s.new, s.lens, s.Hk * s.G, _masks(c.rng, s.new), window=window, pos=pos, pad=1)
 
 
+@pytest.mark.parametrize("new,D", [(5, 64), (40, 128), (70, 256)])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31, 2 ** 32 - 3, 2 ** 33, 2 ** 40, 2 ** 63 - 1])
+def test_windows_wider_than_every_position_are_none(window, new, D):
+    L = _lib()
+    c = _random_cache("i8", 2, 2, D, 6, seed=75)
+    lens, off = _i32([350, 260]), _i32(_offsets([new] * 2))
+    tree = torch.from_numpy(od.words(_masks(c.rng, [new] * 2), 2)).cuda()
+    q = torch.randn(2 * new, 4 * D, device="cuda:0").bfloat16()
+    for pos in (None, _i32(list(range(345, 345 + 2 * new)))):
+        wide = L.readme_attention_kv_tree(0, q, off, lens, *c.args(), 4, tree, pos, window=window)
+        assert torch.equal(wide, L.readme_attention_kv_tree(0, q, off, lens, *c.args(), 4, tree, pos))
+
+
 @pytest.mark.parametrize("D,Hk,G", [(64, 2, 1), (64, 1, 7), (128, 2, 4), (256, 1, 3)])
 @pytest.mark.parametrize("new,lens", [
     ([1], [1]), ([8], [517]), ([64, 65, 63], [64, 200, 127]), ([130, 1, 200], [700, 64, 200]),
