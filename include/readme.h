@@ -1018,13 +1018,15 @@ readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, 
  *   and is then the node, t its p and a = 1.  Otherwise it is refused:
  *     t(v) = max(t(v) - a q(v), 0),  W = sum_v t(v),  a = W / S,
  *   S = 1; or, if distinct = 1 (the drafts of a node were drawn without
- *   replacement), S = the sum of q(v) over the v that were not refused at the node,
- *   and q(x) = 0 from here on (a = 0 if S = 0).  If W = 0, t and a stay as they were
- *   and the node's other drafts are passed over.
+ *   replacement; with q NULL it changes nothing), S = the sum of q(v) over the v
+ *   that were not refused at the node, and q(x) = 0 from here on (a = 0 if S = 0).
+ *   If W = 0, t and a stay as they were and the node's other drafts are passed over.
  *   When no draft is left, the next token is the least v with
  *     t(0) + .. + t(v) > u[row 0] * sum_v t(v).
  * All of it in fp64; p and q as given, neither need sum to 1 exactly; entries that
  * are negative or NaN count as 0, and so do p and q of a token outside [0, V).
+ * Infinite entries, or u outside [0, 1), give an unspecified path and token, the
+ * token still in [0, V) or -1.
  *   dt, p [T][ld_p], q [T][ld_q]  bf16 or fp32; q NULL: the drafts were certain
  *                    (q(v) = 1 at the draft's own token, 0 elsewhere)
  *   tokens, parent [T] int32 (row 0's are not read); u [T] fp32 random numbers in

@@ -1098,12 +1098,13 @@ def readme_verify_drafts(offsets, tokens, parent, p, q, u, distinct: bool = Fals
     token = torch.empty(R, **new) if token is None else token
     one = 16 // p.element_size()
     row = -(-V // one) * one  # the stride of a single row, which has none
-    ld_p, ld_q = _kv_rows(p, T, V, dev, "p") if T > 1 else row, 0
+    ld_p, ld_q = _kv_rows(p, T, V, dev, "p"), 0
     if q is not None:
         if q.dtype is not p.dtype:
             raise ValueError("p and q dtypes disagree")
         ld_q = _kv_rows(q, T, V, dev, "q")
-        ld_q = ld_q if T > 1 else row
+    if T < 2:
+        ld_p = ld_q = row
     if workspace is None:
         ws = readme_verify_drafts_workspace_bytes(T, R, V)
         workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=p.device)

@@ -92,6 +92,14 @@ def test_many_requests_and_refusals(kind):
     assert acc.max() == 1 and (acc == 0).any() and (tok >= 0).all()
 
 
+def test_certain_drafts_are_distinct_or_not_alike():
+    c = Case([1 + i % 9 for i in range(40)], 50, 3, "certain", seed=17, sharp=3.0)
+    L = _lib()
+    args = (_i32(_offsets(c.new)), _i32(c.tokens), _i32(c.parent), c.p, None, torch.from_numpy(c.u).cuda())
+    for a, b in zip(L.readme_verify_drafts(*args), L.readme_verify_drafts(*args, distinct=True)):
+        assert torch.equal(a, b)
+
+
 def test_rows_past_the_limit_are_not_tried():
     c = Case([1500, 1100], 40, 1, seed=5)
     c.u[:] = 0.0   # everything is taken
@@ -272,5 +280,10 @@ def test_python_form_refuses():
                  lambda: L.readme_verify_drafts(off, tok, par, c.p[:, ::2], None, u)):
         with pytest.raises(ValueError):
             call()
+    one = (_i32([0, 1]), tok[:1], par[:1])  # a single row too has its entries side by side
+    with pytest.raises(ValueError):
+        L.readme_verify_drafts(*one, c.p[:, :1].t(), None, u[:1])
+    with pytest.raises(ValueError):
+        L.readme_verify_drafts(*one, c.p[:1, :8], c.q[:, :1].t(), u[:1])
     with pytest.raises(ValueError):
         L.readme_verify_drafts(off, tok, par, c.p.half(), c.q.half(), u)
