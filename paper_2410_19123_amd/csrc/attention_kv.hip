@@ -136,7 +136,25 @@ Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks)
     return {kTilesTile, tile_pairs >= 384 || blocks <= 16 ? 1 : 0};
 }
 
-// The same for rows of draft trees.
+// The same for rows of draft trees, which have a kernel of 32 rows a pair besides, with
+// 1 to 8 waves or in shares.  Measured, us, as above (n drafts for each of so many
+// requests):
+//   shares (more than 64 blocks)
+//     16 x 4 on 16 to 470 blocks    16/0 104, 32/0 112, 128/0 130, 16/4 153
+//     2 x 16 on 470                 32/0 45, 128/0 53, 16/0 75, 32/8 133
+//     1 x 64 on 125                 128/0 36, 32/0 34, 16/8 39
+//     4 x 64 on 940 to 2048         128/0 517, 32/8 617, 32/0 815
+//   whole pairs
+//     16 x 16 on 16 to 64           16/4 41, 32/0 44, 32/4 45, 16/2 63
+//     16 x 32 on 16 to 64           32/4 44, 16/2 58, 128/0 61, 32/2 63
+//     64 x 8 on 8 to 64             16/2 88, 16/4 84, 32/0 83, 16/1 105
+//     128 x 8 on 2 to 8             16/1 32, 16/2 36, 32/1 36
+//     128 x 32 on 2 to 8            32/1 64, 32/2 70, 16/1 83
+//     1 x 64 on 63                  32/8 28, 16/8 24, 32/4 29
+//     40 x 130, four key heads alone, on 16: 32/2 30, 32/1 32, 16/2 39
+//     64 x 32, heads of 64, on 5 to 32: 32/2 28, 32/4 31, 16/2 36
+//     24 x 13 under a window of 18 blocks, heads of 64, seven query heads to each of
+//     four: 32/4 16, 16/4 17, 32/2 21
 Form tree_form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks) {
     if (D == 256) return form_of(T, R, G, Hk, D, blocks);  // 32 rows a wave do not fit the registers
     const int64_t rows = T * G;
@@ -147,7 +165,7 @@ Form tree_form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t bl
     const int tile = rows >= R * 96 ? kTreeTile : kRowsTile;
     const int64_t pairs = (rows + tile - 1) / tile * Hk;
     int w = 1;
-    while (w < 8 && w * 4 <= blocks && pairs * w <= (w == 4 ? 1024 : 2560)) w *= 2;
+    while (w < 8 && w * 4 <= blocks && pairs * w <= (w == 4 ? 1024 : 1280)) w *= 2;
     return {tile, w};
 }
 
