@@ -1107,14 +1107,15 @@ def readme_verify_drafts(offsets, tokens, parent, p, q, u, distinct: bool = Fals
         ld_p = ld_q = row
     if workspace is None:
         ws = readme_verify_drafts_workspace_bytes(T, R, V)
-        workspace = torch.empty(max(ws, 1), dtype=torch.uint8, device=p.device)
+        workspace = torch.empty(ws, dtype=torch.uint8, device=p.device) if ws else None
     _on(dev, workspace, "workspace")
+    ws, bytes_ = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _kv_call(dev, "readme_verify_drafts", _dt(p), T, R, V, _vector(offsets, R + 1, i32, dev, "offsets"),
              _vector(tokens, T, i32, dev, "tokens"), _vector(parent, T, i32, dev, "parent"),
              p.data_ptr(), ld_p, None if q is None else q.data_ptr(), ld_q,
              _vector(u, T, torch.float32, dev, "u"), 1 if distinct else 0,
              _vector(path, T, i32, dev, "path"), _vector(accepted, R, i32, dev, "accepted"),
-             _vector(token, R, i32, dev, "token"), workspace.data_ptr(), workspace.nbytes)
+             _vector(token, R, i32, dev, "token"), ws, bytes_)
     return path, accepted, token
 
 
