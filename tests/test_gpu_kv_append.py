@@ -73,6 +73,40 @@ def test_append_against_the_formula(kt):
     assert (err <= step * (1 + 2.0 ** -20) + 2.0 ** -20 * big).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,Hk,rot,layout,kt,new", [
+    (128, 9, 128, 0, "e4m3", [3001, 1, 0, 64, 2500]), (64, 2, 32, 1, "i8", [9000, 17, 16000, 63, 1]),
+    (128, 4, 48, 1, "i8", [65] * 200), (64, 7, 64, 0, "e4m3", [4000, 3100, 5, 0, 70]),
+    (256, 5, 256, 0, "i8", [6000, 4000, 1, 30, 2])])
+def test_many_rows(D, Hk, rot, layout, kt, new, dtype):
+    """Bit for bit the rotation in fp32 and the write, at sizes where heads share
+    their sines and cosines, on empty blocks and on blocks that hold tokens and grow,
+    with rows of no request and an absent block."""
+    L = _lib()
+    g = torch.Generator().manual_seed(D + Hk)
+    freqs = L.readme_rotary_freqs(rot, device="cuda:0")
+    R, T = len(new), sum(new) + 3
+    mb = -(-(2 * max(new)) // 64) + 1
+    table = torch.randperm(R * mb, generator=g).int().reshape(R, mb)
+    table[0, 1] = -1
+    table = table.cuda()
+    caches = [(torch.zeros((R * mb, Hk, 2, 64 * D), dtype=torch.uint8, device="cuda:0"),
+               torch.zeros((R * mb, Hk, 2), device="cuda:0")) for _ in range(2)]
+    off = _i32(_offsets(new))
+    assert T * Hk >= 49152
+    for step in (1, 2):
+        lens = _i32([step * n for n in new])
+        k, v = (torch.randn((T, Hk * D), generator=g).mul_(step).to(dtype).cuda() for _ in range(2))
+        at = torch.cat([torch.arange((step - 1) * n, step * n) for n in new] + [torch.zeros(3)]).int().cuda()
+        pos = torch.randint(-99, 200000, (T,), generator=g).int().cuda() if step == 2 else None
+        L.readme_kv_append(KT[kt], k, v, off, lens, table, *caches[0], freqs, pos, layout, 1.25)
+        turned = L.readme_rotary(k.float(), at if pos is None else pos, freqs, D, layout, 1.25)
+        L.readme_kv_write(KT[kt], turned, v.float(), off, lens, table, *caches[1])
+        torch.cuda.synchronize()
+        assert torch.equal(caches[0][0], caches[1][0])
+        assert torch.equal(caches[0][1].view(torch.int32), caches[1][1].view(torch.int32))
+
+
 def test_absent_foreign_and_bad_rows():
     """Absent blocks and positions before the first token drop their rows, rows past
     offsets[R] are not read, an infinity turns its block's keys NaN and no other's."""
