@@ -7,8 +7,8 @@
 // the codes.
 // Bound by instructions: 16155 rows of 8 heads of 128, bf16 to e4m3, 99 MB, in 39 us
 // with the angles anew for every head, vector ALU at work in 76% of the busy cycles, and
-// in 34 with sines and cosines shared by four heads, through LDS (through registers, 165
-// of them, 39 to 45); the write alone 29.  K's workgroups come before V's, which are the
+// in 32.5 with sines and cosines shared by four heads, through LDS (69%; through
+// registers, 165 of them, 39 to 45); the write alone 29.  K's workgroups come before V's, which are the
 // shorter: in turns 43 for the 39.  A row each of 64 requests 6.6, the launch and four
 // dependent loads.
 #include "kv_write.hpp"
@@ -152,9 +152,10 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvCacheArgs c, RotaryA
 }
 
 // Of many rows: K of kHeads heads to a workgroup, blockIdx.y < groups, then V of one.
+// Held to 128 registers, four workgroups to a CU: with 138, three, 36 for the 32.5.
 constexpr int kHeads = 4;
 template <int KT, int DT, int D>
-__global__ __launch_bounds__(kKvThreads) void k_kv_append_heads(KvCacheArgs c, RotaryArgs rot, int groups,
+__global__ __launch_bounds__(kKvThreads, 4) void k_kv_append_heads(KvCacheArgs c, RotaryArgs rot, int groups,
                                                                 const void* __restrict__ k, int64_t ld_k,
                                                                 const void* __restrict__ v, int64_t ld_v) {
     __shared__ uint32_t most[4];
@@ -181,10 +182,11 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append_heads(KvCacheArgs c, R
 bool second_apart(const KvCacheArgs& c) { return c.T > c.R && c.R * c.Hk <= 256; }
 
 // Whether four heads share a workgroup, from three units of 64 rows and a head to a CU:
-// us, shared against not (e4m3, heads of 128): 16155 rows of 8 heads 33.8 for 39.8, 8200
-// of 32 65.4 for 73.1, 4096 of 16 19.6 for 22.7, 6144 of 8 18.1 for 19.1; 4096 of 8 17.7
-// for 15.8, 3000 of 8 15.9 for 9.8.  Heads of 64: 24 for 31.  Of 256, whose sines and
-// cosines are 64 KB, 38.7 for 40.2: not worth the kernels.
+// us, shared against not (e4m3, heads of 128): 16155 rows of 8 heads 32.5 for 39.8, 8200
+// of 32 59 for 73, 4096 of 16 20.2 for 22.7, 400 requests of 30 rows 55 for 64, 8 of 768,
+// three units, 18.8 for 19.1; 4096 rows of 8 17.7 for 15.8, 3000 of 8 15.9 for 9.8.  Heads
+// of 64: 25 for 31, at three units 14.6 for 15.9.  Of 256, whose sines and cosines are 64
+// KB, 38.7 for 40.2: not worth the kernels.
 bool heads_share(const KvCacheArgs& c) {
     return c.Hk > 1 && c.Hk <= 32768 && c.T * c.Hk >= 3 * 256 * kKvBlock;  // blockIdx.y below 2^16
 }
