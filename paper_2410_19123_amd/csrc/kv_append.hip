@@ -8,14 +8,27 @@
 // Bound by instructions: 16155 rows of 8 heads of 128, bf16 to e4m3, 99 MB, in 39 us
 // with the angles anew for every head, vector ALU at work in 76% of the busy cycles, and
 // in 32.5 with sines and cosines shared by four heads, through LDS (69%; through
-// registers, 165 of them, 39 to 45); the write alone 29.  K's workgroups come before V's, which are the
-// shorter: in turns 43 for the 39.  A row each of 64 requests 6.6, the launch and four
-// dependent loads.
+// registers, 165 of them, 39 to 45); the write alone 29.  K's workgroups come before
+// V's, which are the shorter: in turns 43 for the 39.  A row each of 64 requests 6.6, the
+// launch and four dependent loads.
 #include "kv_write.hpp"
 
 namespace readme {
 
 namespace {
+
+__device__ __forceinline__ Row16<README_F32> turned_row(const float (&v)[16]) {
+    Row16<README_F32> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        o.v[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                            __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+    return o;
+}
+// The position that a row turns by; a stored one fits 32 bits unless its block is absent.
+__device__ __forceinline__ int position_of(const RotaryArgs& rot, const Touched& b, int row) {
+    return rot.pos ? rot.pos[b.tok + row] : (int)(b.j * kKvBlock + b.slot + row);
+}
 
 // The call's key rows, turned.  The angles' frequencies and the row's position are
 // on their way with the row.
@@ -51,8 +64,7 @@ struct TurnedRows {
         const int64_t at = (b.tok + row) * ld + col;
         load8<DT>(base, at + k.a, x.a);
         load8<DT>(base, at + k.b, x.b);
-        // A stored position fits 32 bits unless its block is absent
-        x.pos = rot.pos ? rot.pos[b.tok + row] : (int)(b.j * kKvBlock + b.slot + row);
+        x.pos = position_of(rot, b, row);
     }
     // Row `row` of the block's rows; zeros past the last.
     __device__ __forceinline__ Row16<README_F32> value(const Raw& x, const Touched& b, int row, int ch) const {
@@ -65,12 +77,7 @@ struct TurnedRows {
             for (int e = 0; e < 8; ++e) t[e] = turn_of((double)x.pos, f[e], rot.amplitude, 1.0f);
             turn_chunk(t, rot.layout, v);
         }
-        Row16<README_F32> o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o.v[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                                __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-        return o;
+        return turned_row(v);
     }
 };
 
@@ -101,7 +108,7 @@ struct KeptRows {
         for (int i = threadIdx.x; i < kItems; i += kKvThreads) {
             const int row = i / (D / 16);
             if (row >= b.n) break;
-            const double pos = (double)(rot.pos ? rot.pos[b.tok + row] : (int)(b.j * kKvBlock + b.slot + row));
+            const double pos = (double)position_of(rot, b, row);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const Turn t = turn_of(pos, f[2 * k], rot.amplitude, 1.0f);
@@ -134,12 +141,7 @@ struct KeptRows {
             }
             turn_chunk(t, rot.layout, v);
         }
-        Row16<README_F32> o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o.v[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                                __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-        return o;
+        return turned_row(v);
     }
 };
 
