@@ -155,6 +155,21 @@ Form form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks)
 //     64 x 32, heads of 64, on 5 to 32: 32/2 28, 32/4 31, 16/2 36
 //     24 x 13 under a window of 18 blocks, heads of 64, seven query heads to each of
 //     four: 32/4 16, 16/4 17, 32/2 21
+//   whole pairs of chains, eight key heads, query heads unshared: a tile holds a request's
+//   few rows and no other's, and what counts is the codes' stream (64 x 5 on 16 to 32
+//   blocks, 201 MB: 4.6 TB/s)
+//     256 x 5 on 4 to 8             16/2 49.6, 16/1 50.3, 16/4 59.9
+//     128 x 5 on 2 to 4             16/1 17, 16/2 19; 40 x 1, 4 x 32 heads: 16/1 18, 16/2 21
+//     64 x 8 on 8 to 16             16/2 23.0, 16/4 24.5, 16/8 32.7
+//     256 x 5 on 8 to 16            16/2 83, 16/4 85, 16/1 91, 16/8 124
+//     64 x 5 on 16 to 32            16/4 44, 16/2 50, 16/1 50, 16/8 53
+//     128 x 1 on 16 to 32           16/2 76, 16/4 76, 16/8 85, 16/1 87
+//     256 x 1 and 256 x 5, the same 16/4 144 and 147, 16/2 146 and 151, 16/1 152 and 163,
+//                                   16/8 158 and 180
+//     128 x 16, the same            16/1 95, 16/2 103, 16/4 107
+//     256 x 5 on 32 to 64           16/4 283, 16/2 290, 16/8 305, 16/1 307
+//     32 x 5, the same              16/4 50, 16/8 53, 16/2 53
+//     16 x 5, the same              16/8 23.0, 16/4 23.5, 16/2 38
 Form tree_form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t blocks) {
     if (D == 256) return form_of(T, R, G, Hk, D, blocks);  // 32 rows a wave do not fit the registers
     const int64_t rows = T * G;
@@ -163,9 +178,16 @@ Form tree_form_of(int64_t T, int64_t R, int64_t G, int64_t Hk, int D, int64_t bl
         return {rows <= R * 64 ? kTreeTile : kTilesTile, 0};
     }
     const int tile = rows >= R * 96 ? kTreeTile : kRowsTile;
-    const int64_t pairs = (rows + tile - 1) / tile * Hk;
+    // A tile never holds rows of two requests: the pairs that run, of requests of equally
+    // many rows, and as many as there would be of full tiles.
+    const int64_t pairs = ceil_div(ceil_div(rows, R), tile) * R * Hk;
+    const int64_t full = ceil_div(rows, tile) * Hk;
     int w = 1;
-    while (w < 8 && w * 4 <= blocks && pairs * w <= (w == 4 ? 1024 : 1280)) w *= 2;
+    while (w < 8 && w * 4 <= blocks && full * w <= 1280) {
+        // Past one round of the chip's waves, four blocks a wave; eight waves only within it
+        if (w == 4 ? pairs > 256 : pairs * w > 1024 && w * 8 > blocks) break;
+        w *= 2;
+    }
     return {tile, w};
 }
 

@@ -13,7 +13,7 @@ namespace {
 constexpr int64_t kMaxRequests = 1 << 22;
 constexpr int64_t kMaxRows = 1 << 27;   // T H / Hk
 // Tiles of 16 query rows times key heads: the attention grids, a workgroup of
-// up to 256 threads for each, stay below 2^32 threads.
+// up to 256 threads for each (of 512 where few run), stay below 2^32 threads.
 constexpr int64_t kMaxPairs = 1 << 23;
 // Every position is below 2^31, and 2^27 rows may lie before the first: a window
 // beyond this is none, and positions less it fit 64 bits.
