@@ -1041,10 +1041,12 @@ readme_status readme_attention_kv_tree(readme_kv_type kt, int64_t T, int32_t R, 
  *                    bytes, then workspace may be NULL), 16-byte aligned, contents
  *                    unspecified before and after; calls in flight together need
  *                    workspaces of their own.
- * p and q are read for the nodes on the path alone.  Rows of a request from
- * README_MAX_DRAFT_ROWS on are not tried.  The taken rows' keys and values lie in
- * the cache behind each other only if the tree was a chain; else they are read
- * (readme_kv_read), and written where they belong with the new lens.
+ * Whole rows of p and q are read for the nodes on the path alone; besides, every
+ * draft's entry of p and q, at its parent's row, is read before the path is known.
+ * What the rows off the path hold, infinities among it, changes nothing.  Rows of
+ * a request from README_MAX_DRAFT_ROWS on are not tried.  The taken rows' keys and
+ * values lie in the cache behind each other only if the tree was a chain; else they
+ * are read (readme_kv_read), and written where they belong with the new lens.
  * T = 0 still writes accepted and token.  Requires 1 <= V < 2^31, T <= 2^27,
  * R <= 2^20, R V <= 2^36, row strides at least V and multiples of 16 bytes, p and q
  * 16-byte aligned, the other arrays 4-byte aligned.
