@@ -193,22 +193,28 @@ bool heads_share(const KvCacheArgs& c) {
     return c.Hk > 1 && c.Hk <= 32768 && c.T * c.Hk >= 3 * 256 * kKvBlock;  // blockIdx.y below 2^16
 }
 
+enum Form : int { kOneByOne, kSecondApart, kHeadsShare };
+Form form_of(const KvCacheArgs& c) {
+    if (c.D < 256 && heads_share(c)) return kHeadsShare;
+    return second_apart(c) ? kSecondApart : kOneByOne;
+}
+
 template <int KT, int DT, int D>
 struct AppendOp {
     static hipError_t go(KvCacheArgs c, RotaryArgs rot, const void* k, int64_t ld_k, const void* v,
                          int64_t ld_v, hipStream_t s) {
+        const Form form = form_of(c);
         if constexpr (D < 256) {
-            if (heads_share(c)) {
+            if (form == kHeadsShare) {
                 const int groups = (c.Hk + kHeads - 1) / kHeads;
                 const dim3 grid(kv_grid(c).x, (unsigned)(groups + c.Hk));
                 k_kv_append_heads<KT, DT, D><<<grid, kKvThreads, 0, s>>>(c, rot, groups, k, ld_k, v, ld_v);
                 return hipGetLastError();
             }
         }
-        const bool apart = second_apart(c);
         dim3 grid = kv_grid(c);
-        if (apart) grid.x += (unsigned)c.R;
-        k_kv_append<KT, DT, D><<<grid, kKvThreads, 0, s>>>(c, rot, apart, k, ld_k, v, ld_v);
+        if (form == kSecondApart) grid.x += (unsigned)c.R;
+        k_kv_append<KT, DT, D><<<grid, kKvThreads, 0, s>>>(c, rot, form == kSecondApart, k, ld_k, v, ld_v);
         return hipGetLastError();
     }
 };
@@ -222,3 +228,14 @@ hipError_t launch_kv_append(readme_kv_type kt, readme_dtype dt, const KvCacheArg
 }
 
 }  // namespace readme
+
+// For the tests: how a call's blocks and heads are dealt to workgroups, 0 one by one, 1
+// second blocks apart, 2 heads sharing sines and cosines.
+extern "C" int32_t readme_internal_kv_append_form(int64_t T, int32_t R, int32_t Hk, int32_t D) {
+    readme::KvCacheArgs c{};
+    c.T = T;
+    c.R = R;
+    c.Hk = Hk;
+    c.D = D;
+    return readme::form_of(c);
+}
