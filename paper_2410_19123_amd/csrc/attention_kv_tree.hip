@@ -11,12 +11,13 @@
 // The codes' conversion to fp16 is paid once for 32 rows.  The waves' sums meet in LDS
 // at the end of a pair.
 //
-// Bound by instructions: a block asks a wave for 32 products of 32 clocks and, for
-// them, about 260 (e4m3) or 512 (int8) conversions and 240 steps of softmax of 4 clocks
-// and more.  16 requests of 32 rows over 1000 to 4096 tokens (heads of 128, four to a
+// Bound by instructions: a block asks a wave (heads of 128) for 32 products of 32 clocks
+// and, for them, 128 (e4m3) or 256 (int8) conversions and about 160 steps of softmax of 4
+// clocks and more.  16 requests of 32 rows over 1000 to 4096 tokens (four query heads to a
 // key head, e4m3): 43 us, of the SIMDs' busy cycles 59% vector ALU and 31% products;
 // the call reads and writes 93 MB, 18 us as a copy, its products are 16 us at a large
 // product's rate; launch, first loads and the join of the waves are 9 of the 43.
+// Two waves a SIMD: 235 to 256 registers, one spilled in three of the e4m3 forms.
 // What did not help, the same call at 45 us: 64 rows a wave, with Q in registers or in
 // LDS, halves the conversions and spills, 90 to 130; a wave's priority raised over its
 // products, and P's sums by dot products, no difference.

@@ -187,8 +187,10 @@ bool second_apart(const KvCacheArgs& c) { return c.T > c.R && c.R * c.Hk <= 256;
 // us, shared against not (e4m3, heads of 128): 16155 rows of 8 heads 32.5 for 39.8, 8200
 // of 32 59 for 73, 4096 of 16 20.2 for 22.7, 400 requests of 30 rows 55 for 64, 8 of 768,
 // three units, 18.8 for 19.1; 4096 rows of 8 17.7 for 15.8, 3000 of 8 15.9 for 9.8.  Heads
-// of 64: 25 for 31, at three units 14.6 for 15.9.  Of 256, whose sines and cosines are 64
-// KB, 38.7 for 40.2: not worth the kernels.
+// of 64: 25 for 31, at three units 14.6 for 15.9.  A row each of 8192 requests, 8 heads,
+// 404 for 467.  Of 256, whose sines and cosines are 64 KB: 8192 rows of 8 heads 38.5 and
+// 39.6 (int8, e4m3) for 41.3 and 41.4, 16160 of 8 66.5 and 71.4 for 68.5 and 71.8, 8192
+// of 4 27 and 29 for 24: not worth the kernels.
 bool heads_share(const KvCacheArgs& c) {
     return c.Hk > 1 && c.Hk <= 32768 && c.T * c.Hk >= 3 * 256 * kKvBlock;  // blockIdx.y below 2^16
 }
